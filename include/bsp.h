@@ -51,7 +51,7 @@ typedef enum {
     BSP_ERR_TIMEOUT = 8    /* a bounded device-side wait expired (latched in the workspace) */
 } bsp_status;
 
-typedef enum { BSP_F32 = 0, BSP_BF16 = 1, BSP_I8 = 2, BSP_I32 = 3 } bsp_dtype;
+typedef enum { BSP_F32 = 0, BSP_BF16 = 1, BSP_I8 = 2, BSP_I32 = 3, BSP_E4M3 = 4, BSP_E5M2 = 5 } bsp_dtype;
 
 /* Block importance (Section "Predetermined Sparsity ratio and Full Training Ahead"). */
 typedef enum { BSP_NORM_L2 = 0, BSP_NORM_L1 = 1, BSP_NORM_VAR = 2 } bsp_norm;
@@ -245,6 +245,64 @@ bsp_status bsp_spgemm(const bsp_wdesc *wa, const bsp_bcsr *a, const bsp_wdesc *w
                       void *stream);
 bsp_status bsp_index_to_relative(int NBo, const int32_t *row_ptr, const int32_t *col_idx, int32_t *rel, void *stream);
 bsp_status bsp_index_from_relative(int NBo, const int32_t *row_ptr, const int32_t *rel, int32_t *col_idx, void *stream);
+
+/* ---- 8-bit floating point: a pruned linear layer's training step and its serving form (Section "Training and Quantization": training
+ * with Gamma; Section "Compiler and its Code generation": 8-bit tensors with power-of-two scales) -------------------
+ * An 8-bit matrix of `rows` rows of `cols` entries: entry (r, k) stands for value(r, k) * 2^(b - 127), where b is the scale byte of row r and
+ * block k / 128 (127: times one; 255: NaN).
+ *   type   BSP_E4M3 (largest value 448) or BSP_E5M2 (57344; the calls below write no infinity)
+ *   data   [rows][bsp_f8_pitch(cols)] bytes, 16-byte aligned; what lies past `cols` in a row is never read
+ *   scale  bsp_f8_scale_bytes() bytes, 16-byte aligned, in the order in which a tensor core takes them: with A = ceil(cols / 512) the byte of
+ *          row r and block b lies at ((r / 128) A + b / 4) 512 + (r % 32) 16 + (r % 128 / 32) 4 + b % 4
+ * The struct is a HOST struct; its pointers are device pointers.  Matrices that a product sums along k need blocks along k, so a tensor that
+ * takes part in two products is quantised in two orientations, "rows" [P][I] and "cols" [I][P], both made from one
+ * reading of it.
+ * bsp_f8_data_bytes / bsp_f8_scale_bytes give 0 for sizes that are not positive. */
+typedef struct {
+    bsp_dtype type;
+    int64_t rows, cols;
+    void *data, *scale;
+} bsp_f8;
+int64_t bsp_f8_pitch(int64_t cols);
+size_t bsp_f8_data_bytes(int64_t rows, int64_t cols);
+size_t bsp_f8_scale_bytes(int64_t rows, int64_t cols);
+
+/* bsp_quantize_f8: X [P][I] (F32 or BF16, rows ldx >= I entries apart) to `rows` (P x I, blocks of 128 entries of a row), to `cols` (I x P, blocks
+ *             of 128 entries of a column) or to both; either may be NULL, not both.  The scale of a block is the smallest power of two, at
+ *             least 2^-127, for which its largest finite entry fits the type; a block of zeros has scale 1.  Entries are divided by
+ *             it (exactly) and rounded once, to nearest even; an infinity or NaN becomes NaN and enters no scale.
+ *             colsum float32 [I], may be NULL: the sums of X's columns, the gradient of a bias (sums of 128 positions, then
+ *             of these, always in the same order).
+ *             ws: bsp_quantize_f8_workspace_bytes() bytes where colsum is given; may be NULL otherwise.
+ * bsp_quantize_weights_f8: Gamma (.) W, W [O][I] of wd->wtype (F32 or BF16; H = K = 1), to `rows` (O x I) and `cols` (I x O) with ONE scale per block of
+ *             128 x 128 entries, so that both hold the same values; either may be NULL, not both.  gamma uint8 [NB_o NB_i] as bsp_mask writes it, NULL for
+ *             all ones; a dropped weight is zero whatever it holds (NaN and infinities included).
+ * bsp_dequantize_f8: the values of m to X (F32 or BF16, rounded to nearest even), X[r][k] or, with transpose != 0, X[k][r]; rows of X ldx entries apart.
+ *             A checkpoint held as `cols` comes back as [P][I] with transpose.
+ * Errors: NULL, SHAPE (sizes not positive or above 2^31 - 1, ldx too small, a form of another size, misaligned pointers; H K != 1), BLOCK, DTYPE, CUDA. */
+size_t bsp_quantize_f8_workspace_bytes(int64_t P, int64_t I);
+bsp_status bsp_quantize_f8(const void *X, bsp_dtype xtype, int64_t P, int64_t I, int64_t ldx, const bsp_f8 *rows, const bsp_f8 *cols, float *colsum,
+                           void *ws, void *stream);
+bsp_status bsp_quantize_weights_f8(const bsp_wdesc *wd, const void *W, const uint8_t *gamma, const bsp_f8 *rows, const bsp_f8 *cols, void *stream);
+bsp_status bsp_dequantize_f8(const bsp_f8 *m, void *X, bsp_dtype xtype, int64_t ldx, int transpose, void *stream);
+
+/* bsp_gemm_f8: Y[m][n] = bias[n] + sum_k x[m][k] w[n][k], x M x K, w N x K (the types may differ), Y dense [M][N] F32 or BF16, 16-byte aligned; bias
+ *             float32 [N], may be NULL.  Forward pass: x = rows form of X, w = rows form of W.  Gradient of the input: x = rows form of dY,
+ *             w = cols form of W.  Products are exact, sums are float32 (in the tensor core, and of up to eight ranges of k, in an
+ *             order that follows from the sizes and the GPU), one rounding to BF16 after the bias.
+ * bsp_gemm_f8_dw: dW[o][i] = Gamma[o / b_o][i / b_i] * sum_p dyt[o][p] xt[i][p], float32 [O][I], 16-byte aligned: the gradient of the kept weights from
+ *             the cols forms of dY (O x P) and of X (I x P, the 8-bit checkpoint of the forward pass); dropped weights get 0 whatever
+ *             the sums are.  gamma may be NULL (all ones).  wd gives O, I and the block shape (its wtype is not used, H = K = 1).
+ * bsp_linear_f8: Y[p][o] = bias[o] + sum_i q(X)[p][i] w[o][i], X [P][I] F32 or BF16 with rows ldx entries apart: bsp_quantize_f8 to e4m3 rows and
+ *             bsp_gemm_f8 in one call, for a layer that only answers (down to a single token).
+ *             ws: bsp_linear_f8_workspace_bytes() bytes.
+ *   ws of the two products: any workspace of at least 256 bytes (status word only).
+ * Errors: NULL, SHAPE (as above; inner sizes differ; sizes of wd differ from the matrices'), BLOCK, DTYPE, CUDA, TIMEOUT (latched). */
+bsp_status bsp_gemm_f8(const bsp_f8 *x, const bsp_f8 *w, const float *bias, void *Y, bsp_dtype ytype, void *ws, void *stream);
+bsp_status bsp_gemm_f8_dw(const bsp_wdesc *wd, const uint8_t *gamma, const bsp_f8 *dyt, const bsp_f8 *xt, float *dW, void *ws, void *stream);
+size_t bsp_linear_f8_workspace_bytes(const bsp_f8 *w, int64_t P);
+bsp_status bsp_linear_f8(const bsp_f8 *w, const void *X, bsp_dtype xtype, int64_t P, int64_t ldx, const float *bias, void *Y, bsp_dtype ytype,
+                         void *ws, void *stream);
 
 /* Synchronises `stream` and returns the status latched in the workspace by the kernels that used it
  * (BSP_OK if none), then clears it. */

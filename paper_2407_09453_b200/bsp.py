@@ -17,14 +17,16 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libbsp.so")
 
 OK, ERR_NULL, ERR_SHAPE, ERR_BLOCK, ERR_DTYPE, ERR_CAPACITY, ERR_INDEX, ERR_CUDA, ERR_TIMEOUT = range(9)
-F32, BF16, I8, I32 = 0, 1, 2, 3
+F32, BF16, I8, I32, E4M3, E5M2 = 0, 1, 2, 3, 4, 5
 NORM_L2, NORM_L1, NORM_VAR = 0, 1, 2
 SCOPE_LAYER, SCOPE_ROW = 0, 1
 
 EXPORTS = ["bsp_mask_workspace_bytes", "bsp_mask", "bsp_mask_static", "bsp_packed_bytes",
            "bsp_compact_workspace_bytes", "bsp_compact_nnz", "bsp_compact", "bsp_conv_workspace_bytes", "bsp_gemm",
            "bsp_conv2d", "bsp_gemm_q8", "bsp_conv2d_q8", "bsp_conv2d_chain", "bsp_conv2d_chain_q8", "bsp_conv_kernel_name", "bsp_spgemm",
-           "bsp_index_to_relative", "bsp_index_from_relative", "bsp_check", "bsp_status_string"]
+           "bsp_index_to_relative", "bsp_index_from_relative", "bsp_f8_pitch", "bsp_f8_data_bytes", "bsp_f8_scale_bytes",
+           "bsp_quantize_f8_workspace_bytes", "bsp_quantize_f8", "bsp_quantize_weights_f8", "bsp_dequantize_f8", "bsp_gemm_f8", "bsp_gemm_f8_dw",
+           "bsp_linear_f8_workspace_bytes", "bsp_linear_f8", "bsp_check", "bsp_status_string"]
 
 
 class BspError(RuntimeError):
@@ -47,16 +49,23 @@ class Bcsr(C.Structure):
                 ("packed", C.c_void_p), ("nnz", C.c_int64)]
 
 
+class F8(C.Structure):
+    _fields_ = [("type", C.c_int), ("rows", C.c_int64), ("cols", C.c_int64), ("data", C.c_void_p), ("scale", C.c_void_p)]
+
+
 # Argument types of the calls that return a status, one letter per argument: p pointer, i int, l int64.  Declared types let
 # the calls below pass plain Python integers and None, which costs a fraction of building a ctypes object per argument.
 _ARG = {"p": C.c_void_p, "i": C.c_int, "l": C.c_int64}
 _ARGS = {"bsp_mask": "ppiilpppp", "bsp_mask_static": "ppiilpp", "bsp_compact_nnz": "ppppp", "bsp_compact": "pppppppl" "pp",
          "bsp_gemm": "ppplppipp", "bsp_conv2d": "ppppppipp", "bsp_gemm_q8": "ppplppppp", "bsp_conv2d_q8": "ppppppppp",
          "bsp_conv2d_chain": "ppppppp" "ippipp", "bsp_conv2d_chain_q8": "pppppppp" "ippppp", "bsp_spgemm": "ppppppp",
-         "bsp_index_to_relative": "ipppp", "bsp_index_from_relative": "ipppp", "bsp_check": "pp"}
+         "bsp_index_to_relative": "ipppp", "bsp_index_from_relative": "ipppp", "bsp_check": "pp",
+         "bsp_quantize_f8": "pilllppppp", "bsp_quantize_weights_f8": "pppppp", "bsp_dequantize_f8": "ppilip", "bsp_gemm_f8": "ppppipp",
+         "bsp_gemm_f8_dw": "ppppppp", "bsp_linear_f8": "ppillppipp"}
 # The functions that csrc/bsp_call.cpp calls, in the order in which it takes their addresses.
 _BOUND = ["bsp_mask", "bsp_compact", "bsp_gemm", "bsp_conv2d", "bsp_gemm_q8", "bsp_conv2d_q8", "bsp_conv2d_chain",
-          "bsp_conv2d_chain_q8", "bsp_spgemm"]
+          "bsp_conv2d_chain_q8", "bsp_spgemm", "bsp_quantize_f8", "bsp_quantize_weights_f8", "bsp_dequantize_f8", "bsp_gemm_f8", "bsp_gemm_f8_dw",
+          "bsp_linear_f8"]
 
 _C_DATA = C.Structure.__mro__[-2]                      # the base of all ctypes objects
 
@@ -72,8 +81,10 @@ def lib():
                                "(or __graft_entry__.build()); there is no CPU fallback")
         L = C.CDLL(LIB_PATH)
         for n in ("bsp_mask_workspace_bytes", "bsp_packed_bytes", "bsp_compact_workspace_bytes",
-                  "bsp_conv_workspace_bytes"):
+                  "bsp_conv_workspace_bytes", "bsp_f8_data_bytes", "bsp_f8_scale_bytes", "bsp_quantize_f8_workspace_bytes",
+                  "bsp_linear_f8_workspace_bytes"):
             getattr(L, n).restype = C.c_size_t
+        L.bsp_f8_pitch.restype = C.c_int64
         L.bsp_status_string.restype = C.c_char_p
         L.bsp_conv_kernel_name.restype = C.c_char_p
         for n, a in _ARGS.items():
@@ -105,7 +116,7 @@ def status_string(status: int) -> str:
     return lib().bsp_status_string(C.c_int(status)).decode()
 
 
-_TORCH_DT = {torch.float32: F32, torch.bfloat16: BF16, torch.int8: I8, torch.int32: I32}
+_TORCH_DT = {torch.float32: F32, torch.bfloat16: BF16, torch.int8: I8, torch.int32: I32, torch.float8_e4m3fn: E4M3, torch.float8_e5m2: E5M2}
 
 
 def dtype_code(t: torch.dtype) -> int:
@@ -224,6 +235,57 @@ def bsp_mask_static(wd: WDesc, W, norm, scope, n_zero, gamma, stream=None):
                                  _stream(stream)), "bsp_mask_static")
 
 
+def bsp_f8_pitch(cols: int) -> int:
+    return int(lib().bsp_f8_pitch(C.c_int64(cols)))
+
+
+def bsp_f8_data_bytes(rows: int, cols: int) -> int:
+    return int(lib().bsp_f8_data_bytes(C.c_int64(rows), C.c_int64(cols)))
+
+
+def bsp_f8_scale_bytes(rows: int, cols: int) -> int:
+    return int(lib().bsp_f8_scale_bytes(C.c_int64(rows), C.c_int64(cols)))
+
+
+def f8matrix(ftype, rows, cols, data, scale) -> F8:
+    """The handle of an 8-bit matrix that lies in tensors of the caller's (bsp_f8 of include/bsp.h says how), which it keeps alive."""
+    m = F8(ftype if isinstance(ftype, int) else dtype_code(ftype), rows, cols, _ptr(data), _ptr(scale))
+    m.tensors = data, scale
+    return m
+
+
+def bsp_quantize_f8_workspace_bytes(P: int, I: int) -> int:
+    return int(lib().bsp_quantize_f8_workspace_bytes(C.c_int64(P), C.c_int64(I)))
+
+
+def bsp_quantize_f8(X, xtype, P, I, ldx, rows: F8 | None, cols: F8 | None, colsum, ws, stream=None):
+    _raise(_native().quantize_f8(X, xtype, P, I, ldx, rows, cols, colsum, ws, stream), "bsp_quantize_f8")
+
+
+def bsp_quantize_weights_f8(wd: WDesc, W, gamma, rows: F8 | None, cols: F8 | None, stream=None):
+    _raise(_native().quantize_weights_f8(wd, W, gamma, rows, cols, stream), "bsp_quantize_weights_f8")
+
+
+def bsp_dequantize_f8(m: F8, X, xtype, ldx, transpose=False, stream=None):
+    _raise(_native().dequantize_f8(m, X, xtype, ldx, 1 if transpose else 0, stream), "bsp_dequantize_f8")
+
+
+def bsp_gemm_f8(x: F8, w: F8, bias, Y, ytype, ws, stream=None):
+    _raise(_native().gemm_f8(x, w, bias, Y, ytype, ws, stream), "bsp_gemm_f8")
+
+
+def bsp_gemm_f8_dw(wd: WDesc, gamma, dyt: F8, xt: F8, dW, ws, stream=None):
+    _raise(_native().gemm_f8_dw(wd, gamma, dyt, xt, dW, ws, stream), "bsp_gemm_f8_dw")
+
+
+def bsp_linear_f8_workspace_bytes(w: F8, P: int) -> int:
+    return int(lib().bsp_linear_f8_workspace_bytes(C.byref(w), C.c_int64(P)))
+
+
+def bsp_linear_f8(w: F8, X, xtype, P, ldx, bias, Y, ytype, ws, stream=None):
+    _raise(_native().linear_f8(w, X, xtype, P, ldx, bias, Y, ytype, ws, stream), "bsp_linear_f8")
+
+
 def bsp_check(ws, stream=None):
     _raise(lib().bsp_check(_ptr(ws), _stream(stream)), "bsp_check")
 
@@ -307,6 +369,88 @@ class SparseLayer:
         if rc is None:
             return bsp_gemm_q8(self.wd, self.handle(), X, X.shape[0], bias, shift, Y, self.ws, stream)
         _raise(rc, "bsp_gemm_q8")
+
+    def check(self, stream=None):
+        bsp_check(self.ws, stream)
+
+
+class F8Matrix:
+    """Device buffers of an 8-bit matrix: `data` [rows][pitch] in the torch type of its format, `scale` bytes, and its handle `m`."""
+
+    def __init__(self, rows, cols, ftype=torch.float8_e4m3fn, device="cuda"):
+        self.rows, self.cols = int(rows), int(cols)
+        self.data = torch.empty((self.rows, bsp_f8_pitch(self.cols)), dtype=ftype, device=device)
+        self.scale = torch.empty(bsp_f8_scale_bytes(self.rows, self.cols), dtype=torch.uint8, device=device)
+        self.m = f8matrix(ftype, self.rows, self.cols, self.data, self.scale)
+
+
+class F8Activations:
+    """Device buffers of P positions of a layer's tensor in 8 bits: `rows` for the next product, `cols` for the weight gradient (the
+    checkpoint that the backward pass reads)."""
+
+    def __init__(self, P, channels, ftype=torch.float8_e4m3fn, device="cuda"):
+        self.rows, self.cols = F8Matrix(P, channels, ftype, device), F8Matrix(channels, P, ftype, device)
+        self.ws = new_workspace(bsp_quantize_f8_workspace_bytes(P, channels), device)
+
+
+def _row_distance(X, what):
+    if X.dim() != 2 or (X.stride(1) != 1 and X.shape[1] > 1):
+        raise ValueError(f"{what}: a matrix whose rows are contiguous is expected")
+    return max(X.stride(0), X.shape[1])
+
+
+def _whole(t, shape, what):
+    if t is not None and (tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+        raise ValueError(f"{what}: a contiguous tensor of shape {tuple(shape)} is expected")
+
+
+class F8Layer:
+    """A pruned linear layer on 8-bit tensors: its weights in both orientations and the calls of a training step and of serving
+    (marshalling only)."""
+
+    def __init__(self, O, I, bo, bi, wtype: torch.dtype, device="cuda"):
+        self.wd = wdesc(O, I, 1, 1, bo, bi, wtype)
+        self.O, self.I, self.device = O, I, device
+        self.w, self.wt = F8Matrix(O, I, device=device), F8Matrix(I, O, device=device)
+        self.gamma = None
+        self.ws = new_workspace(256, device)
+
+    def quantize(self, W, gamma=None, stream=None):
+        """Gamma (.) W in 8 bits; Gamma as SparseLayer.mask leaves it (None: all ones)."""
+        _whole(W, (self.O, self.I), "W")
+        self.gamma = gamma
+        bsp_quantize_weights_f8(self.wd, W, gamma, self.w.m, self.wt.m, stream)
+
+    def linear(self, X, bias, Y, stream=None):
+        """Y = X W^t + bias for a layer that only answers; X in bfloat16 or float32."""
+        P, ldx = X.shape[0], _row_distance(X, "X")
+        if X.shape[1] != self.I:
+            raise ValueError(f"X: {self.I} channels are expected")
+        _whole(Y, (P, self.O), "Y")
+        need = bsp_linear_f8_workspace_bytes(self.w.m, P)
+        if self.ws.numel() < need:
+            self.ws = new_workspace(need, self.device)
+        bsp_linear_f8(self.w.m, X, dtype_code(X.dtype), P, ldx, bias, Y, dtype_code(Y.dtype), self.ws, stream)
+
+    def forward(self, X, act: F8Activations, bias, Y, stream=None):
+        """Y = X W^t + bias; `act` holds X in 8 bits afterwards."""
+        _whole(Y, (X.shape[0], self.O), "Y")
+        bsp_quantize_f8(X, dtype_code(X.dtype), X.shape[0], X.shape[1], _row_distance(X, "X"), act.rows.m, act.cols.m, None, act.ws, stream)
+        bsp_gemm_f8(act.rows.m, self.w.m, bias, Y, dtype_code(Y.dtype), self.ws, stream)
+
+    def backward(self, dY, act: F8Activations, grad: F8Activations, dX=None, dW=None, db=None, stream=None):
+        """Gradients of the input, of the kept weights and of the bias (those that are given) from dY and the checkpoint in `act`; `grad`
+        holds dY in 8 bits afterwards."""
+        P = dY.shape[0]
+        _whole(dX, (P, self.I), "dX")
+        _whole(dW, (self.O, self.I), "dW")
+        _whole(db, (self.O,), "db")
+        bsp_quantize_f8(dY, dtype_code(dY.dtype), P, dY.shape[1], _row_distance(dY, "dY"), grad.rows.m if dX is not None or dW is None else None,
+                        grad.cols.m if dW is not None else None, db, grad.ws, stream)
+        if dX is not None:
+            bsp_gemm_f8(grad.rows.m, self.wt.m, None, dX, dtype_code(dX.dtype), self.ws, stream)
+        if dW is not None:
+            bsp_gemm_f8_dw(self.wd, self.gamma, grad.cols.m, act.cols.m, dW, self.ws, stream)
 
     def check(self, stream=None):
         bsp_check(self.ws, stream)

@@ -2,6 +2,7 @@
 // stream.  Declarations and their contracts are in include/bsp.h.
 #include <cstdio>
 #include <cstdlib>
+#include "bsp_f8.cuh"
 #include "bsp_internal.cuh"
 
 namespace bsp {
@@ -231,6 +232,140 @@ bsp_status bsp_gemm(const bsp_wdesc *wd, const bsp_bcsr *w, const void *X, int64
     if (P <= 0 || P > 0x7FFFFFFF) return BSP_ERR_SHAPE;
     bsp_xdesc xd = {(int)P, 1, 1, 1, 1, 0, 0};
     return bsp_conv2d(wd, w, &xd, X, bias, Y, ytype, ws, stream);
+}
+
+// ---- 8-bit floating point ----
+
+int64_t bsp_f8_pitch(int64_t cols) { return cols > 0 ? f8_pitch(cols) : 0; }
+size_t bsp_f8_data_bytes(int64_t rows, int64_t cols) { return rows > 0 && cols > 0 ? (size_t)rows * (size_t)f8_pitch(cols) : 0; }
+size_t bsp_f8_scale_bytes(int64_t rows, int64_t cols) { return rows > 0 && cols > 0 ? (size_t)f8_scale_bytes(rows, cols) : 0; }
+
+namespace {
+constexpr int64_t kF8Most = 0x7FFFFFFF;
+
+bsp_status check_f8(const bsp_f8 *m)
+{
+    if (!m) return BSP_ERR_NULL;
+    if (m->type != BSP_E4M3 && m->type != BSP_E5M2) return BSP_ERR_DTYPE;
+    if (m->rows <= 0 || m->cols <= 0 || m->rows > kF8Most || m->cols > kF8Most) return BSP_ERR_SHAPE;
+    if (!m->data || !m->scale) return BSP_ERR_NULL;
+    if (!aligned16(m->data) || !aligned16(m->scale)) return BSP_ERR_SHAPE;
+    return BSP_OK;
+}
+// Rows of a plain tensor: type, sizes, distance of rows, alignment to elements.
+bsp_status check_plain(const void *X, bsp_dtype t, int64_t rows, int64_t cols, int64_t ldx)
+{
+    if (t != BSP_F32 && t != BSP_BF16) return BSP_ERR_DTYPE;
+    if (!X) return BSP_ERR_NULL;
+    if (rows <= 0 || cols <= 0 || rows > kF8Most || cols > kF8Most || ldx < cols) return BSP_ERR_SHAPE;
+    if ((uintptr_t)X % elem_bytes(t) != 0) return BSP_ERR_SHAPE;
+    return BSP_OK;
+}
+// The forms that a quantiser fills: `rows` R x C, `cols` C x R, of one type.
+bsp_status check_forms(const bsp_f8 *rows, const bsp_f8 *cols, int64_t R, int64_t C)
+{
+    if (!rows && !cols) return BSP_ERR_NULL;
+    if (rows) {
+        const bsp_status rc = check_f8(rows);
+        if (rc != BSP_OK) return rc;
+        if (rows->rows != R || rows->cols != C) return BSP_ERR_SHAPE;
+    }
+    if (cols) {
+        const bsp_status rc = check_f8(cols);
+        if (rc != BSP_OK) return rc;
+        if (cols->rows != C || cols->cols != R) return BSP_ERR_SHAPE;
+    }
+    if (rows && cols && rows->type != cols->type) return BSP_ERR_DTYPE;
+    return BSP_OK;
+}
+bsp_status check_product(const bsp_f8 *x, const bsp_f8 *w, const float *bias, const void *Y, bsp_dtype ytype, const void *ws)
+{
+    bsp_status rc = check_f8(x);
+    if (rc == BSP_OK) rc = check_f8(w);
+    if (rc != BSP_OK) return rc;
+    if (!Y || !ws) return BSP_ERR_NULL;
+    if (ytype != BSP_F32 && ytype != BSP_BF16) return BSP_ERR_DTYPE;
+    if (x->cols != w->cols || !aligned16(Y) || (bias && !aligned4(bias))) return BSP_ERR_SHAPE;
+    return BSP_OK;
+}
+}  // namespace
+
+size_t bsp_quantize_f8_workspace_bytes(int64_t P, int64_t I)
+{
+    if (P <= 0 || I <= 0) return 0;
+    return kWsHeader + align_up((size_t)f8_blocks(P) * (size_t)I * 4, 256);
+}
+
+bsp_status bsp_quantize_f8(const void *X, bsp_dtype xtype, int64_t P, int64_t I, int64_t ldx, const bsp_f8 *rows, const bsp_f8 *cols, float *colsum,
+                           void *ws, void *stream)
+{
+    bsp_status rc = check_plain(X, xtype, P, I, ldx);
+    if (rc == BSP_OK) rc = check_forms(rows, cols, P, I);
+    if (rc != BSP_OK) return rc;
+    if (colsum && !ws) return BSP_ERR_NULL;
+    if (colsum && !aligned4(colsum)) return BSP_ERR_SHAPE;
+    return launch_quantize_f8(X, xtype, P, I, ldx, nullptr, nullptr, rows, cols, colsum, ws, (cudaStream_t)stream);
+}
+
+bsp_status bsp_quantize_weights_f8(const bsp_wdesc *wd, const void *W, const uint8_t *gamma, const bsp_f8 *rows, const bsp_f8 *cols, void *stream)
+{
+    bsp_status rc = check_wdesc(wd);
+    if (rc != BSP_OK) return rc;
+    if (wd->H != 1 || wd->K != 1) return BSP_ERR_SHAPE;
+    rc = check_plain(W, wd->wtype, wd->O, wd->I, wd->I);
+    if (rc == BSP_OK) rc = check_forms(rows, cols, wd->O, wd->I);
+    if (rc != BSP_OK) return rc;
+    return launch_quantize_f8(W, wd->wtype, wd->O, wd->I, wd->I, wd, gamma, rows, cols, nullptr, nullptr, (cudaStream_t)stream);
+}
+
+bsp_status bsp_dequantize_f8(const bsp_f8 *m, void *X, bsp_dtype xtype, int64_t ldx, int transpose, void *stream)
+{
+    bsp_status rc = check_f8(m);
+    if (rc != BSP_OK) return rc;
+    rc = transpose ? check_plain(X, xtype, m->cols, m->rows, ldx) : check_plain(X, xtype, m->rows, m->cols, ldx);
+    if (rc != BSP_OK) return rc;
+    return launch_dequantize_f8(*m, X, xtype, ldx, transpose != 0, (cudaStream_t)stream);
+}
+
+bsp_status bsp_gemm_f8(const bsp_f8 *x, const bsp_f8 *w, const float *bias, void *Y, bsp_dtype ytype, void *ws, void *stream)
+{
+    const bsp_status rc = check_product(x, w, bias, Y, ytype, ws);
+    if (rc != BSP_OK) return rc;
+    return launch_gemm_f8(*x, *w, bias, nullptr, nullptr, Y, ytype, ws, (cudaStream_t)stream);
+}
+
+bsp_status bsp_gemm_f8_dw(const bsp_wdesc *wd, const uint8_t *gamma, const bsp_f8 *dyt, const bsp_f8 *xt, float *dW, void *ws, void *stream)
+{
+    bsp_status rc = check_wdesc(wd);
+    if (rc != BSP_OK) return rc;
+    if (wd->H != 1 || wd->K != 1) return BSP_ERR_SHAPE;
+    rc = check_product(dyt, xt, nullptr, dW, BSP_F32, ws);
+    if (rc != BSP_OK) return rc;
+    if (dyt->rows != wd->O || xt->rows != wd->I) return BSP_ERR_SHAPE;
+    return launch_gemm_f8(*dyt, *xt, nullptr, wd, gamma, dW, BSP_F32, ws, (cudaStream_t)stream);
+}
+
+size_t bsp_linear_f8_workspace_bytes(const bsp_f8 *w, int64_t P)
+{
+    if (!w || w->cols <= 0 || P <= 0) return 0;
+    return kWsHeader + align_up(bsp_f8_data_bytes(P, w->cols), 256) + bsp_f8_scale_bytes(P, w->cols);
+}
+
+bsp_status bsp_linear_f8(const bsp_f8 *w, const void *X, bsp_dtype xtype, int64_t P, int64_t ldx, const float *bias, void *Y, bsp_dtype ytype,
+                         void *ws, void *stream)
+{
+    bsp_status rc = check_f8(w);
+    if (rc != BSP_OK) return rc;
+    rc = check_plain(X, xtype, P, w->cols, ldx);
+    if (rc != BSP_OK) return rc;
+    if (!ws) return BSP_ERR_NULL;
+    uint8_t *at = (uint8_t *)ws + kWsHeader;
+    const bsp_f8 x = {BSP_E4M3, P, w->cols, at, at + align_up(bsp_f8_data_bytes(P, w->cols), 256)};
+    rc = check_product(&x, w, bias, Y, ytype, ws);
+    if (rc != BSP_OK) return rc;
+    rc = launch_quantize_f8(X, xtype, P, w->cols, ldx, nullptr, nullptr, &x, nullptr, nullptr, ws, (cudaStream_t)stream);
+    if (rc != BSP_OK) return rc;
+    return launch_gemm_f8(x, *w, bias, nullptr, nullptr, Y, ytype, ws, (cudaStream_t)stream);
 }
 
 bsp_status bsp_check(void *ws, void *stream)

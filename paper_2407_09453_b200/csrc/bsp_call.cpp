@@ -91,6 +91,9 @@ T *structure(PyObject *o)
 template <class T>
 T convert(PyObject *o)
 {
+    if constexpr (std::is_same_v<T, const bsp_f8 *>)
+        return o == Py_None ? nullptr : structure<bsp_f8>(o);
+    else
     if constexpr (std::is_same_v<T, const bsp_wdesc *> || std::is_same_v<T, const bsp_xdesc *> || std::is_same_v<T, const bsp_bcsr *>)
         return structure<std::remove_pointer_t<T>>(o);
     else if constexpr (std::is_pointer_v<T>)
@@ -110,6 +113,12 @@ decltype(&bsp_conv2d_q8) f_conv2d_q8;
 decltype(&bsp_conv2d_chain) f_chain;
 decltype(&bsp_conv2d_chain_q8) f_chain_q8;
 decltype(&bsp_spgemm) f_spgemm;
+decltype(&bsp_quantize_f8) f_quantize_f8;
+decltype(&bsp_quantize_weights_f8) f_quantize_weights_f8;
+decltype(&bsp_dequantize_f8) f_dequantize_f8;
+decltype(&bsp_gemm_f8) f_gemm_f8;
+decltype(&bsp_gemm_f8_dw) f_gemm_f8_dw;
+decltype(&bsp_linear_f8) f_linear_f8;
 
 // Runs a body that may raise; the status of the library's call as a Python integer.
 template <class F>
@@ -169,6 +178,12 @@ BSP_CALL(conv2d_q8, f_conv2d_q8)
 BSP_CALL(conv2d_chain, f_chain)
 BSP_CALL(conv2d_chain_q8, f_chain_q8)
 BSP_CALL(spgemm, f_spgemm)
+BSP_CALL(quantize_f8, f_quantize_f8)
+BSP_CALL(quantize_weights_f8, f_quantize_weights_f8)
+BSP_CALL(dequantize_f8, f_dequantize_f8)
+BSP_CALL(gemm_f8, f_gemm_f8)
+BSP_CALL(gemm_f8_dw, f_gemm_f8_dw)
+BSP_CALL(linear_f8, f_linear_f8)
 #undef BSP_CALL
 
 // ---- the calls of SparseLayer: the handle, the input's shape and the output's type are read here ----
@@ -259,11 +274,11 @@ PyObject *layer_conv2d(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// bind(c_data, mask, compact, gemm, conv2d, gemm_q8, conv2d_q8, chain, chain_q8, spgemm): the base of ctypes objects and the addresses
-// of the loaded library's functions
+// bind(c_data, mask, compact, gemm, conv2d, gemm_q8, conv2d_q8, chain, chain_q8, spgemm, quantize_f8, quantize_weights_f8, dequantize_f8, gemm_f8,
+// gemm_f8_dw, linear_f8): the base of ctypes objects and the addresses of the loaded library's functions
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    if (!count_is(n, 10)) return nullptr;
+    if (!count_is(n, 16)) return nullptr;
     return guarded([&] {
         if (!PyType_Check(a[0])) {
             PyErr_SetString(PyExc_TypeError, "not a type");
@@ -280,6 +295,12 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
         f_chain = (decltype(f_chain))integer(a[7]);
         f_chain_q8 = (decltype(f_chain_q8))integer(a[8]);
         f_spgemm = (decltype(f_spgemm))integer(a[9]);
+        f_quantize_f8 = (decltype(f_quantize_f8))integer(a[10]);
+        f_quantize_weights_f8 = (decltype(f_quantize_weights_f8))integer(a[11]);
+        f_dequantize_f8 = (decltype(f_dequantize_f8))integer(a[12]);
+        f_gemm_f8 = (decltype(f_gemm_f8))integer(a[13]);
+        f_gemm_f8_dw = (decltype(f_gemm_f8_dw))integer(a[14]);
+        f_linear_f8 = (decltype(f_linear_f8))integer(a[15]);
         return 0;
     });
 }
@@ -287,7 +308,8 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 #define BSP_DEF(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {BSP_DEF(bind), BSP_DEF(mask), BSP_DEF(compact), BSP_DEF(gemm), BSP_DEF(conv2d), BSP_DEF(gemm_q8), BSP_DEF(conv2d_q8),
                          BSP_DEF(conv2d_chain), BSP_DEF(conv2d_chain_q8), BSP_DEF(spgemm), BSP_DEF(fill_handle), BSP_DEF(layer_gemm),
-                         BSP_DEF(layer_conv2d), {nullptr, nullptr, 0, nullptr}};
+                         BSP_DEF(layer_conv2d), BSP_DEF(quantize_f8), BSP_DEF(quantize_weights_f8), BSP_DEF(dequantize_f8), BSP_DEF(gemm_f8),
+                         BSP_DEF(gemm_f8_dw), BSP_DEF(linear_f8), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_bspcall", "Argument marshalling of bsp.py.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }   // namespace

@@ -1,0 +1,362 @@
+// To 8-bit floating point and back: activations and gradients with one power-of-two scale for 128 entries along the axis that a
+// product sums over, weights Gamma (.) W with one scale per block of 128 x 128, each in both orientations from one pass over the
+// input; column sums (the gradient of a bias) beside them.  Section "Compiler and its Code generation" (8-bit tensors with
+// power-of-two scales) and Section "Training and Quantization" of the paper.
+//
+// A block's scale is 2^e with the smallest e for which its largest entry fits the format, so x 2^-e is exact and an entry is rounded
+// once, to the format.  A tile of 128 x 128 entries is one block of scales in either orientation: a CTA reads it once into
+// registers (thread (tx, ty) holds rows 8 ty .. 8 ty + 7 of columns 8 tx .. 8 tx + 7), finds the largest entry of every row by shuffles
+// and of every column through shared memory, and writes both forms, the transposed one through shared memory so that its rows
+// leave in pieces of 128 bytes.  Bound by HBM: e + 2 bytes an entry.
+#include "bsp_f8.cuh"
+
+namespace bsp {
+namespace {
+
+constexpr int kQThreads = 256;
+
+struct QParams {
+    const void *X;
+    int64_t P, I, ldx;
+    int vec;                      // rows of X can be read 16 bytes at a time
+    uint8_t *rows, *rows_scale, *cols, *cols_scale;
+    int64_t rows_pitch, cols_pitch, rows_atoms, cols_atoms;
+    float *partial;               // column sums of every tile of 128 positions, [P / 128][I]
+    const uint8_t *gamma;         // weights: Gamma, or NULL for all ones
+    int bo, bi;
+    int64_t NBi;
+    int64_t tiles_i;
+};
+
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// Eight entries of one row, zeros past the end.
+template <typename T>
+__device__ __forceinline__ void q_load8(const T *row, int64_t c, int64_t I, int vec, float (&v)[8])
+{
+    if (vec && c + 8 <= I) {
+        if constexpr (sizeof(T) == 2) {
+            const uint4 w = load_free((const uint4 *)(row + c));
+            v[0] = bf16_lo(w.x); v[1] = bf16_hi(w.x); v[2] = bf16_lo(w.y); v[3] = bf16_hi(w.y);
+            v[4] = bf16_lo(w.z); v[5] = bf16_hi(w.z); v[6] = bf16_lo(w.w); v[7] = bf16_hi(w.w);
+        } else {
+            const float4 a = load_free((const float4 *)(row + c)), b = load_free<16>((const float4 *)(row + c));
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = c + i < I ? (float)row[c + i] : 0.f;
+    }
+}
+
+template <typename T, bool kE5, bool kWeights>
+__global__ void __launch_bounds__(kQThreads) quantize_f8_kernel(const QParams p)
+{
+    __shared__ __align__(16) uint8_t s_cols[kF8Block * kF8Block];
+    __shared__ float s_max[8][kF8Block], s_sum[8][kF8Block];
+    __shared__ __align__(16) float s_inv[kF8Block];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, tx = tid & 15, ty = tid >> 4;
+    const int64_t ti = (int64_t)blockIdx.x % p.tiles_i, tp = (int64_t)blockIdx.x / p.tiles_i;
+    const int64_t c0 = ti * kF8Block + tx * 8, r0 = tp * kF8Block + ty * 8;
+    wait_for_previous();
+    const T *X = from_here((const T *)p.X);
+
+    float v[8][8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if (r0 + j < p.P && c0 < p.I) q_load8(X + (r0 + j) * p.ldx, c0, p.I, p.vec, v[j]);
+        else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[j][i] = 0.f;
+    }
+    if constexpr (kWeights) {
+        // a block of Gamma covers whole groups of four rows and of four columns, whatever its shape; dropped weights are zeros, whatever
+        // they hold
+        if (p.gamma != nullptr) {
+            const uint8_t *gamma = from_here(p.gamma);
+#pragma unroll
+            for (int jh = 0; jh < 8; jh += 4)
+#pragma unroll
+                for (int ih = 0; ih < 8; ih += 4) {
+                    const bool keep = r0 + jh < p.P && c0 + ih < p.I && load_free(gamma + (r0 + jh) / p.bo * p.NBi + (c0 + ih) / p.bi) != 0u;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[jh + j][ih + i] = keep ? v[jh + j][ih + i] : 0.f;
+                }
+        }
+    }
+    if (p.partial != nullptr) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float s = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s += v[j][i];
+            s += __shfl_xor_sync(0xFFFFFFFFu, s, 16);
+            if (lane < 16) s_sum[warp][tx * 8 + i] = s;
+        }
+    }
+
+    // Largest entries of the rows (over the 16 lanes that share them).  fmaxf passes by NaN; an infinity becomes NaN first, so that it neither
+    // enters a scale nor comes out as the format's largest value.
+    float rmax[8];
+    auto find_rows = [&]() {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float m = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[j][i]));
+#pragma unroll
+            for (int d = 8; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+            rmax[j] = m;
+        }
+    };
+    find_rows();
+    bool inf = false;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) inf |= rmax[j] == __uint_as_float(0x7F800000u);
+    if (__any_sync(0xFFFFFFFFu, inf)) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (fabsf(v[j][i]) == __uint_as_float(0x7F800000u)) v[j][i] = __uint_as_float(0x7FFFFFFFu);
+        find_rows();
+    }
+    if constexpr (kWeights) {
+        // one scale for the tile
+        float m = rmax[0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j) m = fmaxf(m, rmax[j]);
+        m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
+        if (lane == 0) s_max[0][warp] = m;
+        __syncthreads();
+        m = s_max[0][0];
+#pragma unroll
+        for (int w = 1; w < 8; ++w) m = fmaxf(m, s_max[0][w]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) rmax[j] = m;
+    } else if (p.cols != nullptr) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float m = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(v[j][i]));
+            m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
+            if (lane < 16) s_max[warp][tx * 8 + i] = m;
+        }
+    }
+
+    // rows form: eight bytes a thread and row, 128 bytes a row of the tile
+    if (p.rows != nullptr) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t b = f8_scale_byte<kE5>(__float_as_uint(rmax[j]));
+            const float f = f8_inverse(b);
+            uint2 w;
+            w.x = f8_pack<kE5>(v[j][0] * f, v[j][1] * f) | f8_pack<kE5>(v[j][2] * f, v[j][3] * f) << 16;
+            w.y = f8_pack<kE5>(v[j][4] * f, v[j][5] * f) | f8_pack<kE5>(v[j][6] * f, v[j][7] * f) << 16;
+            if (r0 + j < p.P && c0 < p.rows_pitch) *(uint2 *)(p.rows + (r0 + j) * p.rows_pitch + c0) = w;
+            if (tx == 0) p.rows_scale[f8_scale_at(r0 + j, ti, p.rows_atoms)] = (uint8_t)b;      // (the scales reach whole groups of 128 rows)
+        }
+    }
+    if (p.cols == nullptr && p.partial == nullptr) return;
+    __syncthreads();
+    if (tid < kF8Block) {
+        const int64_t c = ti * kF8Block + tid;
+        if (p.cols != nullptr) {
+            float m = rmax[0];
+            if constexpr (!kWeights) {
+                m = s_max[0][tid];
+#pragma unroll
+                for (int w = 1; w < 8; ++w) m = fmaxf(m, s_max[w][tid]);
+            }
+            const uint32_t b = f8_scale_byte<kE5>(__float_as_uint(m));
+            s_inv[tid] = f8_inverse(b);
+            p.cols_scale[f8_scale_at(c, tp, p.cols_atoms)] = (uint8_t)b;
+        }
+        if (p.partial != nullptr && c < p.I) {
+            float s = s_sum[0][tid];
+#pragma unroll
+            for (int w = 1; w < 8; ++w) s += s_sum[w][tid];
+            p.partial[tp * p.I + c] = s;
+        }
+    }
+    if (p.cols == nullptr) return;
+    __syncthreads();
+    // transposed form: the eight bytes of a column's rows to shared memory, 8-byte piece ty of column c at place ty ^ (c / 8) so that the
+    // lanes of a half warp, eight columns apart, meet different banks
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float f = s_inv[tx * 8 + i];
+        uint2 w;
+        w.x = f8_pack<kE5>(v[0][i] * f, v[1][i] * f) | f8_pack<kE5>(v[2][i] * f, v[3][i] * f) << 16;
+        w.y = f8_pack<kE5>(v[4][i] * f, v[5][i] * f) | f8_pack<kE5>(v[6][i] * f, v[7][i] * f) << 16;
+        *(uint2 *)(s_cols + (tx * 8 + i) * kF8Block + ((ty ^ tx) << 3)) = w;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const int piece = u * kQThreads + tid, col = piece >> 3, at = piece & 7, x = col >> 3;
+        const int64_t c = ti * kF8Block + col, r = tp * kF8Block + at * 16;
+        uint4 w = *(const uint4 *)(s_cols + col * kF8Block + ((at ^ (x >> 1)) << 4));
+        if (x & 1) w = make_uint4(w.z, w.w, w.x, w.y);
+        if (c < p.I && r < p.cols_pitch) *(uint4 *)(p.cols + c * p.cols_pitch + r) = w;
+    }
+}
+
+// Sums of the tiles' column sums, in the order of the tiles.
+__global__ void __launch_bounds__(256) colsum_kernel(const float *partial, int64_t tiles, int64_t I, float *out)
+{
+    __shared__ float s[8][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t c = (int64_t)blockIdx.x * 32 + lane;
+    wait_for_previous();
+    partial = from_here(partial);
+    float sum = 0.f;
+    if (c < I)
+        for (int64_t t = warp; t < tiles; t += 8) sum += __uint_as_float(load_free((const uint32_t *)(partial + t * I + c)));
+    s[warp][lane] = sum;
+    __syncthreads();
+    if (warp == 0 && c < I) {
+#pragma unroll
+        for (int w = 1; w < 8; ++w) sum += s[w][lane];
+        out[c] = sum;
+    }
+}
+
+// ---- back ----
+
+struct DParams {
+    const uint8_t *data, *scale;
+    int64_t rows, cols, pitch, atoms, ldx, tiles;
+    void *X;
+    int vec;
+};
+
+// Eight entries in a row of X; `n` of them exist.
+__device__ __forceinline__ void d_store8(__nv_bfloat16 *x, const float (&v)[8], int n, int vec)
+{
+    if (vec && n >= 8) {
+        uint4 w;
+        uint32_t *o = &w.x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+            o[i] = *(const uint32_t *)&h;
+        }
+        *(uint4 *)x = w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) x[i] = __float2bfloat16_rn(v[i]);
+    }
+}
+__device__ __forceinline__ void d_store8(float *x, const float (&v)[8], int n, int vec)
+{
+    if (vec && n >= 8) {
+        *(float4 *)x = make_float4(v[0], v[1], v[2], v[3]);
+        *(float4 *)(x + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) x[i] = v[i];
+    }
+}
+
+// A tile of 128 x 128 per CTA.  A thread takes 8 x 8 entries; a warp 64 rows x 32 columns, so that it reads 32 bytes of a row at once and
+// writes, transposed, 64 consecutive entries of a row of X.
+template <typename T, bool kE5, bool kTranspose>
+__global__ void __launch_bounds__(256) dequantize_f8_kernel(const DParams p)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int tx = kTranspose ? (warp & 3) * 4 + (lane & 3) : lane & 15, ty = kTranspose ? (warp >> 2) * 8 + (lane >> 2) : warp * 2 + (lane >> 4);
+    const int64_t tk = (int64_t)blockIdx.x % p.tiles, tr = (int64_t)blockIdx.x / p.tiles;
+    const int64_t k0 = tk * kF8Block + tx * 8, r0 = tr * kF8Block + ty * 8;
+    wait_for_previous();
+    if (k0 >= p.cols || r0 >= p.rows) return;
+    const uint8_t *data = from_here(p.data), *scale = from_here(p.scale);
+    const int nk = p.cols - k0 < 8 ? (int)(p.cols - k0) : 8, nr = p.rows - r0 < 8 ? (int)(p.rows - r0) : 8;
+    uint2 w[8];
+    float f[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        w[j] = j < nr ? load_free((const uint2 *)(data + (r0 + j) * p.pitch + k0)) : make_uint2(0u, 0u);
+        f[j] = j < nr ? f8_scale(load_free(scale + f8_scale_at(r0 + j, tk, p.atoms))) : 0.f;
+    }
+    T *X = (T *)p.X;
+    if constexpr (!kTranspose) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (j >= nr) break;
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 a = f8_unpack<kE5>((i < 2 ? w[j].x : w[j].y) >> (16 * (i & 1)) & 0xFFFFu);
+                v[2 * i] = a.x * f[j]; v[2 * i + 1] = a.y * f[j];
+            }
+            d_store8(X + (r0 + j) * p.ldx + k0, v, nk, p.vec);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            float a[8], b[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float2 t = f8_unpack<kE5>((i < 4 ? w[j].x : w[j].y) >> (8 * (i & 2)) & 0xFFFFu);
+                a[j] = t.x * f[j]; b[j] = t.y * f[j];
+            }
+            if (i < nk) d_store8(X + (k0 + i) * p.ldx + r0, a, nr, p.vec);
+            if (i + 1 < nk) d_store8(X + (k0 + i + 1) * p.ldx + r0, b, nr, p.vec);
+        }
+    }
+}
+
+bool rows_of_16(const void *X, int64_t ldx, int esz) { return ((uintptr_t)X & 15u) == 0 && ldx * esz % 16 == 0; }
+
+}  // namespace
+
+bsp_status launch_quantize_f8(const void *X, bsp_dtype xtype, int64_t P, int64_t I, int64_t ldx, const bsp_wdesc *wd, const uint8_t *gamma,
+                              const bsp_f8 *rows, const bsp_f8 *cols, float *colsum, void *ws, cudaStream_t st)
+{
+    QParams p = {};
+    p.X = X; p.P = P; p.I = I; p.ldx = ldx;
+    p.vec = rows_of_16(X, ldx, elem_bytes(xtype));
+    if (rows) { p.rows = (uint8_t *)rows->data; p.rows_scale = (uint8_t *)rows->scale; p.rows_pitch = f8_pitch(I); p.rows_atoms = f8_atoms(I); }
+    if (cols) { p.cols = (uint8_t *)cols->data; p.cols_scale = (uint8_t *)cols->scale; p.cols_pitch = f8_pitch(P); p.cols_atoms = f8_atoms(P); }
+    if (colsum) p.partial = (float *)((char *)ws + kWsHeader);
+    if (wd) { p.gamma = gamma; p.bo = wd->bo; p.bi = wd->bi; p.NBi = wd->I / wd->bi; }
+    p.tiles_i = f8_blocks(I);
+    const int64_t tiles_p = f8_blocks(P), tiles = p.tiles_i * tiles_p;
+    if (tiles > 0x7FFFFFFF) return BSP_ERR_SHAPE;
+    const bool e5 = (rows ? rows->type : cols ? cols->type : BSP_E4M3) == BSP_E5M2, half = xtype == BSP_BF16;
+    typedef void (*Kernel)(const QParams);
+    static const Kernel kernels[2][2][2] = {
+        {{quantize_f8_kernel<float, false, false>, quantize_f8_kernel<float, false, true>}, {quantize_f8_kernel<float, true, false>, quantize_f8_kernel<float, true, true>}},
+        {{quantize_f8_kernel<__nv_bfloat16, false, false>, quantize_f8_kernel<__nv_bfloat16, false, true>},
+         {quantize_f8_kernel<__nv_bfloat16, true, false>, quantize_f8_kernel<__nv_bfloat16, true, true>}}};
+    BSP_CUDA_OK(launch_after(kernels[half][e5][wd != nullptr], dim3((unsigned)tiles), dim3(kQThreads), 0, st, p));
+    if (colsum) BSP_CUDA_OK(launch_after(colsum_kernel, dim3((unsigned)((I + 31) / 32)), dim3(256), 0, st, (const float *)p.partial, tiles_p, I, colsum));
+    return BSP_OK;
+}
+
+bsp_status launch_dequantize_f8(const bsp_f8 &m, void *X, bsp_dtype xtype, int64_t ldx, bool transpose, cudaStream_t st)
+{
+    DParams p = {};
+    p.data = (const uint8_t *)m.data; p.scale = (const uint8_t *)m.scale;
+    p.rows = m.rows; p.cols = m.cols; p.pitch = f8_pitch(m.cols); p.atoms = f8_atoms(m.cols); p.ldx = ldx; p.X = X;
+    p.vec = rows_of_16(X, ldx, elem_bytes(xtype));
+    p.tiles = f8_blocks(m.cols);
+    const int64_t tiles = p.tiles * f8_blocks(m.rows);
+    if (tiles > 0x7FFFFFFF) return BSP_ERR_SHAPE;
+    typedef void (*Kernel)(const DParams);
+    static const Kernel kernels[2][2][2] = {
+        {{dequantize_f8_kernel<float, false, false>, dequantize_f8_kernel<float, false, true>}, {dequantize_f8_kernel<float, true, false>, dequantize_f8_kernel<float, true, true>}},
+        {{dequantize_f8_kernel<__nv_bfloat16, false, false>, dequantize_f8_kernel<__nv_bfloat16, false, true>},
+         {dequantize_f8_kernel<__nv_bfloat16, true, false>, dequantize_f8_kernel<__nv_bfloat16, true, true>}}};
+    BSP_CUDA_OK(launch_after(kernels[xtype == BSP_BF16][m.type == BSP_E5M2][transpose], dim3((unsigned)tiles), dim3(256), 0, st, p));
+    return BSP_OK;
+}
+
+}  // namespace bsp

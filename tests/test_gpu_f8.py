@@ -1,0 +1,348 @@
+"""GPU parity of the 8-bit floating-point operators against the numpy oracle: quantised matrices bit for bit in both orientations, products
+within the bound that their additions have (f8_util.product_bound)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import f8
+from paper_2407_09453_b200 import bsp, synth
+from f8_util import FTYPE, XTYPE, codes_of, device, held, product_bound, random_held, values
+
+pytestmark = pytest.mark.gpu
+
+
+def quantize_both(X, ftype, colsum=None, ldx=None):
+    P, I = X.shape
+    act = bsp.F8Activations(P, I, FTYPE[ftype])
+    for m in (act.rows, act.cols):
+        m.data.view(torch.uint8).fill_(0xEE)
+        m.scale.fill_(0xEE)
+    bsp.bsp_quantize_f8(X, bsp.dtype_code(X.dtype), P, I, I if ldx is None else ldx, act.rows.m, act.cols.m, colsum, act.ws)
+    return act
+
+
+def assert_forms(act, x, ftype):
+    for m, t in ((act.rows, x), (act.cols, x.T)):
+        codes, scales = f8.quantize(t, ftype)
+        got_codes, got_scales = codes_of(m)
+        assert np.array_equal(got_scales, scales)
+        assert np.array_equal(got_codes, codes)
+
+
+@pytest.mark.parametrize("P,I,dtype,ftype", [(1, 8, "bf16", "e4m3"), (1, 1, "f32", "e5m2"), (128, 128, "bf16", "e4m3"), (127, 129, "f32", "e4m3"), (130, 200, "bf16", "e5m2"),
+                                             (64, 2048, "bf16", "e4m3"), (5, 1003, "bf16", "e4m3"), (300, 77, "f32", "e5m2"), (1023, 264, "bf16", "e4m3")])
+def test_quantize_both_orientations(P, I, dtype, ftype):
+    x = values(2000 + P, P, I, dtype)
+    act = quantize_both(device(x, dtype), ftype)
+    assert_forms(act, x, ftype)
+
+
+def test_quantize_one_orientation_leaves_the_other():
+    x = values(2100, 140, 300, "bf16")
+    X = device(x, "bf16")
+    for which in ("rows", "cols"):
+        act = bsp.F8Activations(140, 300)
+        other = act.cols if which == "rows" else act.rows
+        other.data.view(torch.uint8).fill_(0xAB)
+        bsp.bsp_quantize_f8(X, bsp.BF16, 140, 300, 300, act.rows.m if which == "rows" else None, act.cols.m if which == "cols" else None, None, None)
+        codes, scales = f8.quantize(x if which == "rows" else x.T, "e4m3")
+        got = codes_of(getattr(act, which))
+        assert np.array_equal(got[0], codes) and np.array_equal(got[1], scales)
+        assert bool((other.data.view(torch.uint8) == 0xAB).all())
+
+
+@pytest.mark.parametrize("dtype,off,ldx", [("bf16", 0, 264), ("bf16", 3, 261), ("f32", 0, 260), ("f32", 1, 259), ("bf16", 8, 512)])
+def test_quantize_strides_and_alignment(dtype, off, ldx):
+    """Rows that are not packed and buffers that start off a 16-byte boundary; what lies between the rows is not read as data."""
+    P, I = 133, 250
+    x = values(2200 + off, P, I, dtype)
+    store = torch.full((P * ldx + off,), float("nan"), dtype=XTYPE[dtype], device="cuda")
+    view = torch.as_strided(store, (P, I), (ldx, 1), off)
+    view.copy_(device(x, dtype))
+    act = quantize_both(view, "e4m3", None, ldx)
+    assert_forms(act, x, "e4m3")
+
+
+@pytest.mark.parametrize("ftype", ["e4m3", "e5m2"])
+def test_quantize_extremes(ftype):
+    """Blocks of zeros, NaN and infinities (NaN in 8 bits, in no scale), subnormals, the largest floats, entries exactly at a scale's border."""
+    x = values(2300, 256, 384, "f32")
+    x[0] = 0.0
+    x[:, 1] = 0.0
+    x[3, 5], x[3, 200], x[7, 300] = np.nan, np.inf, -np.inf
+    x[9] = np.nan
+    x[11] = np.inf
+    x[13] = 2.0 ** -149
+    x[15] = np.finfo(np.float32).max
+    x[17, :128] = f8.MAX[ftype]
+    x[18, :128] = np.nextafter(np.float32(f8.MAX[ftype]), np.float32(np.inf))
+    x[19, :128] = np.float32(2.0 ** -126)
+    act = quantize_both(device(x, "f32"), ftype)
+    assert_forms(act, x, ftype)
+
+
+@pytest.mark.parametrize("P,I,dtype", [(1, 16, "bf16"), (129, 100, "f32"), (1500, 513, "bf16")])
+def test_column_sums(P, I, dtype):
+    x = values(2400 + P, P, I, dtype)
+    sums = torch.full((I,), float("nan"), device="cuda")
+    act = quantize_both(device(x, dtype), "e4m3", sums)
+    assert_forms(act, x, "e4m3")
+    want = x.astype(np.float64).sum(0)
+    # a sum of P terms, at most 8 + 16 + tiles additions deep, each off by half a step of what can have been summed
+    depth = 8 + 1 + 8 + -(-P // 1024) + 8
+    assert (np.abs(sums.cpu().numpy() - want) <= depth * 2.0 ** -24 * np.abs(x.astype(np.float64)).sum(0) * 1.01).all()
+    again = torch.empty_like(sums)
+    bsp.bsp_quantize_f8(device(x, dtype), bsp.dtype_code(XTYPE[dtype]), P, I, I, act.rows.m, None, again, act.ws)
+    assert torch.equal(again, sums)                                       # always the same order
+
+
+@pytest.mark.parametrize("O,I,bo,bi,dtype", [(8, 8, 8, 8, "bf16"), (136, 264, 8, 8, "f32"), (1000, 304, 4, 16, "bf16"), (272, 132, 16, 4, "f32"), (128, 128, 8, 8, "bf16")])
+def test_quantize_weights(O, I, bo, bi, dtype):
+    w = values(2500 + O, O, I, dtype, 0.05)
+    gamma = synth.random_gamma(2501, O // bo, I // bi, (O // bo) * (I // bi) // 2)
+    gamma[0] = 0                                                           # a row of Gamma that keeps nothing
+    hidden = np.where(f8.spread_gamma(gamma, O, I, bo, bi), w, np.where(np.arange(I) % 3 == 0, np.nan, np.inf)).astype(np.float32)
+    lay = bsp.F8Layer(O, I, bo, bi, XTYPE[dtype])
+    g = torch.from_numpy(np.ascontiguousarray(gamma, dtype=np.uint8)).cuda()
+    lay.quantize(device(hidden, dtype), g)
+    want = f8.masked(w.astype(np.float64), gamma, bo, bi)
+    codes, scales = f8.quantize(want, "e4m3", 128)
+    got = codes_of(lay.w)
+    assert np.array_equal(got[1], scales) and np.array_equal(got[0] & 0x7F, codes & 0x7F)
+    back = f8.dequantize(*got, "e4m3")
+    assert np.array_equal(back, f8.dequantize(codes, scales, "e4m3"))
+    assert np.array_equal(f8.dequantize(*codes_of(lay.wt), "e4m3"), back.T)      # both orientations hold the same values
+    lay.quantize(device(w, dtype))
+    codes, scales = f8.quantize(w, "e4m3", 128)
+    got = codes_of(lay.w)
+    assert np.array_equal(got[0], codes) and np.array_equal(got[1], scales)
+
+
+@pytest.mark.parametrize("R,K,dtype,ftype", [(1, 1, "f32", "e4m3"), (130, 260, "bf16", "e4m3"), (257, 100, "f32", "e5m2"), (33, 1000, "bf16", "e5m2")])
+@pytest.mark.parametrize("transpose", [False, True])
+def test_dequantize(R, K, dtype, ftype, transpose):
+    codes, scales = f8.quantize(values(2600 + R, R, K, "f32"), ftype)
+    m = held(codes, scales, ftype)
+    shape = (K, R) if transpose else (R, K)
+    ld = shape[1] + 5
+    store = torch.full((shape[0], ld), -7.0, dtype=XTYPE[dtype], device="cuda")
+    bsp.bsp_dequantize_f8(m.m, store, bsp.dtype_code(XTYPE[dtype]), ld, transpose)
+    want = f8.dequantize(codes, scales, ftype)
+    got = store.float().cpu().numpy()
+    assert np.array_equal(got[:, :shape[1]], (want.T if transpose else want).astype(np.float32))     # (a value has few bits: bf16 holds it)
+    assert (got[:, shape[1]:] == -7.0).all()
+
+
+def test_dequantize_every_code_and_scale():
+    for ftype in ("e4m3", "e5m2"):
+        codes = np.tile(np.arange(256, dtype=np.uint8), (256, 1))
+        scales = np.repeat(np.arange(256, dtype=np.uint8)[:, None], 2, axis=1)
+        m = held(codes, scales, ftype)
+        X = torch.empty((256, 256), device="cuda")
+        bsp.bsp_dequantize_f8(m.m, X, bsp.F32, 256)
+        with np.errstate(over="ignore", invalid="ignore"):
+            want = f8.dequantize(codes, scales, ftype).astype(np.float32)
+        want[255] = np.nan
+        assert np.array_equal(X.cpu().numpy(), want, equal_nan=True)
+
+
+def gemm(A, a, B, b, bias, out):
+    M, N = a.shape[0], b.shape[0]
+    ws = bsp.new_workspace(256)
+    guard = 64
+    store = torch.full((M * N + guard,), -7.0, dtype=XTYPE[out], device="cuda")
+    Y = store[:M * N].view(M, N)
+    bsp.bsp_gemm_f8(A.m, B.m, None if bias is None else torch.from_numpy(bias).cuda(), Y, bsp.dtype_code(XTYPE[out]), ws)
+    bsp.bsp_check(ws)
+    want = a @ b.T + (0.0 if bias is None else bias.astype(np.float64))
+    got = Y.float().cpu().numpy()
+    assert bool((store[M * N:] == -7.0).all())
+    return got, want
+
+
+@pytest.mark.parametrize("M,N,K,at,bt,out", [
+    (1, 8, 16, "e4m3", "e4m3", "f32"), (1, 1, 1, "e4m3", "e4m3", "f32"), (128, 128, 128, "e4m3", "e4m3", "f32"), (3, 5, 200, "e5m2", "e4m3", "f32"),
+    (16, 128, 512, "e4m3", "e4m3", "bf16"), (17, 136, 640, "e4m3", "e5m2", "f32"), (33, 257, 1000, "e4m3", "e4m3", "bf16"), (64, 1000, 2048, "e4m3", "e4m3", "f32"),
+    (65, 24, 130, "e5m2", "e5m2", "f32"), (129, 300, 1024, "e4m3", "e4m3", "f32"), (1000, 264, 8192, "e5m2", "e4m3", "f32"), (1023, 2048, 384, "e4m3", "e4m3", "bf16"),
+    (1, 4096, 4096, "e4m3", "e4m3", "f32"), (20000, 128, 72, "e4m3", "e4m3", "bf16")])
+def test_gemm(M, N, K, at, bt, out):
+    A, a = random_held(3000 + M, M, K, at)
+    B, b = random_held(3100 + N, N, K, bt, 0.05)
+    bias = synth.normal(3200, (N,), 1.0).astype(np.float32)
+    got, want = gemm(A, a, B, b, bias, out)
+    assert (np.abs(got - want) <= product_bound(a, b, want, out)).all()
+    got, want = gemm(A, a, B, b, None, out)
+    assert (np.abs(got - want) <= product_bound(a, b, want, out)).all()
+
+
+def test_gemm_scales_across_their_range():
+    """Scales that differ from row to row and block to block by up to 2^80."""
+    M, N, K = 200, 150, 700
+    codes, _ = f8.quantize(values(3300, M, K, "f32"), "e4m3")
+    wcodes, _ = f8.quantize(values(3301, N, K, "f32"), "e4m3")
+    s, t = synth.uniform_int(3302, (M, 6), 87, 167).astype(np.uint8), synth.uniform_int(3303, (N, 6), 87, 167).astype(np.uint8)
+    a, b = f8.dequantize(codes, s, "e4m3"), f8.dequantize(wcodes, t, "e4m3")
+    got, want = gemm(held(codes, s, "e4m3"), a, held(wcodes, t, "e4m3"), b, None, "f32")
+    assert (np.abs(got - want) <= product_bound(a, b, want, "f32")).all()
+
+
+def test_gemm_nan_stays_in_its_row_and_column():
+    M, N, K = 150, 140, 260
+    codes, s = f8.quantize(values(3400, M, K, "f32"), "e4m3")
+    wcodes, t = f8.quantize(values(3401, N, K, "f32"), "e4m3")
+    codes[5, 259], wcodes[131, 0] = 0x7F, 0xFF
+    A, B = held(codes, s, "e4m3"), held(wcodes, t, "e4m3")
+    a, b = f8.dequantize(codes, s, "e4m3"), f8.dequantize(wcodes, t, "e4m3")
+    got, _ = gemm(A, a, B, b, None, "f32")
+    assert np.isnan(got[5]).all() and np.isnan(got[:, 131]).all()
+    rows, cols = np.arange(M) != 5, np.arange(N) != 131
+    a, b = a[rows], b[cols]
+    want = a @ b.T
+    assert (np.abs(got[rows][:, cols] - want) <= product_bound(a, b, want, "f32")).all()
+
+
+@pytest.mark.parametrize("O,I,P,bo,bi,at", [(8, 8, 1, 8, 8, "e4m3"), (64, 64, 333, 8, 8, "e5m2"), (256, 80, 5000, 4, 16, "e4m3"), (144, 260, 129, 16, 4, "e5m2"),
+                                            (1024, 256, 1000, 8, 8, "e4m3")])
+def test_weight_gradient(O, I, P, bo, bi, at):
+    A, a = random_held(3500 + O, O, P, at, 1e-3)
+    B, b = random_held(3600 + I, I, P, "e4m3")
+    gamma = synth.random_gamma(3700, O // bo, I // bi, (O // bo) * (I // bi) // 2)
+    wd, ws = bsp.wdesc(O, I, 1, 1, bo, bi, bsp.F32), bsp.new_workspace(256)
+    for g in (gamma, None):
+        dW = torch.full((O, I), float("nan"), device="cuda")
+        bsp.bsp_gemm_f8_dw(wd, None if g is None else torch.from_numpy(np.ascontiguousarray(g, dtype=np.uint8)).cuda(), A.m, B.m, dW, ws)
+        bsp.bsp_check(ws)
+        want = f8.masked(a @ b.T, g, bo, bi)
+        got = dW.cpu().numpy()
+        assert (np.abs(got - want) <= product_bound(a, b, want, "f32")).all()
+        if g is not None:
+            assert (got[~f8.spread_gamma(g, O, I, bo, bi)] == 0).all()
+
+
+def test_weight_gradient_of_dropped_blocks_is_zero_even_where_sums_are_nan():
+    O, I, P = 64, 64, 200
+    codes, s = f8.quantize(values(3800, O, P, "f32"), "e5m2")
+    codes[:] = 0x7F
+    xcodes, t = f8.quantize(values(3801, I, P, "f32"), "e4m3")
+    gamma = synth.random_gamma(3802, 8, 8, 40)
+    dW = torch.full((O, I), 3.0, device="cuda")
+    ws = bsp.new_workspace(256)
+    bsp.bsp_gemm_f8_dw(bsp.wdesc(O, I, 1, 1, 8, 8, bsp.BF16), torch.from_numpy(np.ascontiguousarray(gamma, dtype=np.uint8)).cuda(), held(codes, s, "e5m2").m, held(xcodes, t, "e4m3").m, dW, ws)
+    keep = f8.spread_gamma(gamma, O, I, 8, 8)
+    got = dW.cpu().numpy()
+    assert np.isnan(got[keep]).all() and (got[~keep] == 0).all()
+
+
+@pytest.mark.parametrize("P,I,O,dtype,out", [(1, 8, 8, "bf16", "f32"), (1, 4096, 1000, "bf16", "bf16"), (7, 1003, 72, "f32", "f32"), (16, 512, 640, "bf16", "f32"), (33, 264, 40, "f32", "bf16"),
+                                             (64, 2048, 1000, "f32", "f32"), (200, 136, 264, "bf16", "bf16")])
+def test_linear(P, I, O, dtype, out):
+    x = values(3900 + P, P, I, dtype)
+    B, b = random_held(3901 + O, O, I, "e4m3", 0.05)
+    a = f8.dequantize(*f8.quantize(x, "e4m3"), "e4m3")
+    bias = synth.normal(3902, (O,), 1.0).astype(np.float32)
+    ldx = I + 8
+    X = torch.full((P, ldx), float("nan"), dtype=XTYPE[dtype], device="cuda")
+    X[:, :I] = device(x, dtype)
+    Y = torch.full((P, O), -7.0, dtype=XTYPE[out], device="cuda")
+    ws = bsp.new_workspace(bsp.bsp_linear_f8_workspace_bytes(B.m, P))
+    bsp.bsp_linear_f8(B.m, X, bsp.dtype_code(XTYPE[dtype]), P, ldx, torch.from_numpy(bias).cuda(), Y, bsp.dtype_code(XTYPE[out]), ws)
+    bsp.bsp_check(ws)
+    want = a @ b.T + bias.astype(np.float64)
+    assert (np.abs(Y.float().cpu().numpy() - want) <= product_bound(a, b, want, out)).all()
+
+
+def step_tensors(P, O, I):
+    w, x, dy = values(4000, O, I, "f32", 0.05), values(4001, P, I, "bf16"), values(4002, P, O, "bf16", 1e-3)
+    bias = synth.normal(4003, (O,), 1.0).astype(np.float32)
+    return w, x, dy, bias
+
+
+def test_training_step_with_gamma_from_the_mask_builder():
+    """Mask, quantised weights, forward, backward as a program runs them; the gradients against the formulas and against differences of the
+    loss sum(Y dY) of the layer that the 8-bit tensors define (which is linear, so a difference is exact but for rounding)."""
+    P, O, I = 700, 264, 392
+    w, x, dy, bias = step_tensors(P, O, I)
+    W, X, dY, b = device(w, "f32"), device(x, "bf16"), device(dy, "bf16"), torch.from_numpy(bias).cuda()
+    prune = bsp.SparseLayer(O, I, 1, 1, 8, 8, torch.float32)
+    prune.mask(W, (O // 8) * (I // 8) // 2)
+    lay = bsp.F8Layer(O, I, 8, 8, torch.float32)
+    act, grad = bsp.F8Activations(P, I), bsp.F8Activations(P, O, torch.float8_e5m2)
+    Y, dX, dW, db = torch.empty((P, O), device="cuda"), torch.empty((P, I), dtype=torch.bfloat16, device="cuda"), torch.empty((O, I), device="cuda"), torch.empty(O, device="cuda")
+    lay.quantize(W, prune.gamma)
+    lay.forward(X, act, b, Y)
+    lay.backward(dY, act, grad, dX, dW, db)
+    lay.check()
+    gamma = prune.gamma.cpu().numpy()
+    keep = f8.spread_gamma(gamma, O, I, 8, 8)
+    back = lambda t, f, rows=1: f8.dequantize(*f8.quantize(t, f, rows), f)  # noqa: E731
+    wq, xq, xqt = back(f8.masked(w.astype(np.float64), gamma, 8, 8), "e4m3", 128), back(x, "e4m3"), back(x.T, "e4m3")
+    gq, gqt = back(dy, "e5m2"), back(dy.T, "e5m2")
+    for got, want, p, q, out in ((Y, xq @ wq.T + bias.astype(np.float64), xq, wq, "f32"), (dX, gq @ wq, gq, wq.T, "bf16"), (dW, np.where(keep, gqt @ xqt.T, 0.0), gqt, xqt, "f32")):
+        assert (np.abs(got.float().cpu().numpy() - want) <= product_bound(p, q, want, out)).all()
+    assert (np.abs(db.cpu().numpy() - dy.astype(np.float64).sum(0)) <= 40 * 2.0 ** -24 * np.abs(dy.astype(np.float64)).sum(0)).all()
+    # differences: loss(W) = sum over p of (xhat W^t) . dyhat in 64 bits, with the tensors' own 8-bit values
+    loss = lambda m: float(((xqt.T @ m.T) * gqt.T).sum())  # noqa: E731
+    for o, i in ((0, 0), (100, 200), (263, 391)):
+        for k in range(8):
+            o1, i1 = o // 8 * 8 + k, i // 8 * 8 + k
+            d = np.zeros_like(wq)
+            d[o1, i1] = 1.0 if keep[o1, i1] else 0.0
+            diff = (loss(d) - loss(-d)) / 2
+            bound = product_bound(gqt[o1:o1 + 1], xqt[i1:i1 + 1], np.array([[diff]]), "f32")[0, 0]
+            assert abs(float(dW[o1, i1]) - diff) <= bound + 1e-9 * abs(diff)
+
+
+def test_step_is_captured_into_a_graph_and_replayed_on_new_inputs():
+    P, O, I = 130, 136, 264
+    w, x, dy, bias = step_tensors(P, O, I)
+    lay = bsp.F8Layer(O, I, 8, 8, torch.float32)
+    act, grad = bsp.F8Activations(P, I), bsp.F8Activations(P, O, torch.float8_e5m2)
+    W, X, dY, b = device(w, "f32"), device(x, "bf16"), device(dy, "bf16"), torch.from_numpy(bias).cuda()
+    Y, dX, dW, db = torch.empty((P, O), device="cuda"), torch.empty((P, I), device="cuda"), torch.empty((O, I), device="cuda"), torch.empty(O, device="cuda")
+
+    def step():
+        lay.quantize(W)
+        lay.forward(X, act, b, Y)
+        lay.backward(dY, act, grad, dX, dW, db)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    X.copy_(device(values(4100, P, I, "bf16"), "bf16"))
+    W.copy_(device(values(4101, O, I, "f32", 0.05), "f32"))
+    graph.replay()
+    torch.cuda.synchronize()
+    got = [t.clone() for t in (Y, dX, dW, db)]
+    for t in (Y, dX, dW, db):
+        t.fill_(float("nan"))
+    step()
+    lay.check()
+    assert all(torch.equal(a, b) for a, b in zip(got, (Y, dX, dW, db)))
+
+
+def test_calls_of_two_streams_side_by_side():
+    """Layers with workspaces of their own on two streams, many calls deep: each gives what it gives alone."""
+    P, O, I = 64, 1000, 1024
+    lays, outs, xs, alone = [], [], [], []
+    for k in range(2):
+        lay = bsp.F8Layer(O, I, 8, 8, torch.float32)
+        lay.quantize(device(values(4200 + k, O, I, "f32", 0.05), "f32"))
+        X = device(values(4210 + k, P, I, "bf16"), "bf16")
+        Y = torch.empty((P, O), device="cuda")
+        lay.linear(X, None, Y)
+        torch.cuda.synchronize()
+        lays.append(lay); xs.append(X); outs.append([torch.empty_like(Y) for _ in range(20)]); alone.append(Y.clone())
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for n in range(20):
+        for k in range(2):
+            lays[k].linear(xs[k], None, outs[k][n], streams[k])
+    torch.cuda.synchronize()
+    for k in range(2):
+        lays[k].check()
+        assert all(torch.equal(y, alone[k]) for y in outs[k])

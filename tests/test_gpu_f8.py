@@ -175,6 +175,29 @@ def test_gemm(M, N, K, at, bt, out):
     assert (np.abs(got - want) <= product_bound(a, b, want, out)).all()
 
 
+@pytest.mark.parametrize("M,N,K,at,bt,out", [(2300, 2056, 400, "e4m3", "e4m3", "bf16"), (2300, 2056, 4400, "e5m2", "e4m3", "f32"), (20000, 264, 136, "e4m3", "e5m2", "f32"),
+                                             (130, 20000, 2048, "e4m3", "e4m3", "bf16"), (2049, 2564, 2050, "e4m3", "e4m3", "f32")])
+def test_gemm_large(M, N, K, at, bt, out):
+    """Products that take pairs of CTAs: ragged in both directions, one and several sums of 2048 entries, more tiles than pairs."""
+    A, a = random_held(3050 + M, M, K, at)
+    B, b = random_held(3150 + N, N, K, bt, 0.05)
+    bias = synth.normal(3250, (N,), 1.0).astype(np.float32)
+    got, want = gemm(A, a, B, b, bias, out)
+    assert (np.abs(got - want) <= product_bound(a, b, want, out)).all()
+
+
+def test_weight_gradient_large():
+    O, I, P = 2304, 2312, 2700
+    A, a = random_held(3510, O, P, "e5m2", 1e-3)
+    B, b = random_held(3610, I, P, "e4m3")
+    gamma = synth.random_gamma(3710, O // 8, I // 8, (O // 8) * (I // 8) // 2)
+    dW, ws = torch.full((O, I), float("nan"), device="cuda"), bsp.new_workspace(256)
+    bsp.bsp_gemm_f8_dw(bsp.wdesc(O, I, 1, 1, 8, 8, bsp.F32), torch.from_numpy(np.ascontiguousarray(gamma, dtype=np.uint8)).cuda(), A.m, B.m, dW, ws)
+    bsp.bsp_check(ws)
+    want = f8.masked(a @ b.T, gamma, 8, 8)
+    assert (np.abs(dW.cpu().numpy() - want) <= product_bound(a, b, want, "f32")).all()
+
+
 def test_gemm_scales_across_their_range():
     """Scales that differ from row to row and block to block by up to 2^80."""
     M, N, K = 200, 150, 700

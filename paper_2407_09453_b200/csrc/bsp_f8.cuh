@@ -14,6 +14,8 @@ __host__ __device__ inline int64_t f8_blocks(int64_t cols) { return (cols + kF8B
 __host__ __device__ inline int64_t f8_atoms(int64_t cols) { return (f8_blocks(cols) + 3) / 4; }
 inline int64_t f8_scale_bytes(int64_t rows, int64_t cols) { return f8_blocks(rows) * f8_atoms(cols) * kF8Atom; }
 
+inline int f8_log2(int block) { return block == 4 ? 2 : block == 8 ? 3 : 4; }      // sides of Gamma's blocks
+
 // Place of the scale of row r and block b among the scales of a matrix with `atoms` atoms per 128 rows: the order in which
 // tcgen05.cp takes 128 rows to 32 lanes of tensor memory (row r to lane r % 32, column r / 32, four blocks to a column's bytes).
 __host__ __device__ inline int64_t f8_scale_at(int64_t r, int64_t b, int64_t atoms)

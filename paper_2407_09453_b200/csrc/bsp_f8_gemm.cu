@@ -563,8 +563,6 @@ bsp_status fp_scale_map(CUtensorMap *map, const bsp_f8 &m, int box_blocks)
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? BSP_OK : BSP_ERR_CUDA;
 }
 
-int log2_of(int block) { return block == 4 ? 2 : block == 8 ? 3 : 4; }
-
 bsp_status launch_pairs(const bsp_f8 &x, const bsp_f8 &w, const float *bias, const bsp_wdesc *wd, const uint8_t *gamma, void *Y, bsp_dtype ytype, void *ws,
                         int sms, cudaStream_t st)
 {
@@ -579,7 +577,7 @@ bsp_status launch_pairs(const bsp_f8 &x, const bsp_f8 &w, const float *bias, con
     // formats, N / 8, scales of 8 exponent bits, M / 128
     p.idesc = ((x.type == BSP_E5M2 ? 1u : 0u) << 7) | ((w.type == BSP_E5M2 ? 1u : 0u) << 10) | (32u << 17) | (1u << 23) | (2u << 27);
     p.bias = bias;
-    if (wd) { p.gamma = gamma; p.bo = log2_of(wd->bo); p.bi = log2_of(wd->bi); p.NBi = wd->I / wd->bi; }
+    if (wd) { p.gamma = gamma; p.bo = f8_log2(wd->bo); p.bi = f8_log2(wd->bi); p.NBi = wd->I / wd->bi; }
     p.status = (int *)ws;
     bsp_status rc = fs_map(&p.tma, x, 128);
     if (rc == BSP_OK) rc = fs_map(&p.tmb, w, 128);

@@ -23,52 +23,148 @@ struct QParams {
     int64_t rows_pitch, cols_pitch, rows_atoms, cols_atoms;
     float *partial;               // column sums of every tile of 128 positions, [P / 128][I]
     const uint8_t *gamma;         // weights: Gamma, or NULL for all ones
-    int bo, bi;
+    int bo, bi;                   // logarithms of the sizes of Gamma's blocks
     int64_t NBi;
     int64_t tiles_i;
 };
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
-
-// Eight entries of one row, zeros past the end.
-template <typename T>
-__device__ __forceinline__ void q_load8(const T *row, int64_t c, int64_t I, int vec, float (&v)[8])
+__device__ __forceinline__ uint32_t bf16_max2(uint32_t a, uint32_t b)      // (passes by NaN)
 {
-    if (vec && c + 8 <= I) {
-        if constexpr (sizeof(T) == 2) {
-            const uint4 w = load_free((const uint4 *)(row + c));
-            v[0] = bf16_lo(w.x); v[1] = bf16_hi(w.x); v[2] = bf16_lo(w.y); v[3] = bf16_hi(w.y);
-            v[4] = bf16_lo(w.z); v[5] = bf16_hi(w.z); v[6] = bf16_lo(w.w); v[7] = bf16_hi(w.w);
-        } else {
-            const float4 a = load_free((const float4 *)(row + c)), b = load_free<16>((const float4 *)(row + c));
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = c + i < I ? (float)row[c + i] : 0.f;
-    }
+    const __nv_bfloat162 m = __hmax2(*(const __nv_bfloat162 *)&a, *(const __nv_bfloat162 *)&b);
+    return *(const uint32_t *)&m;
 }
 
+// 8 x 8 entries in registers, bfloat16 as they come (two to a word), so that three CTAs fit an SM.
+template <typename T>
+struct QEntries {
+    static constexpr int kWords = sizeof(T) == 2 ? 4 : 8;          // words of eight entries
+    uint32_t w[8][kWords];
+
+    __device__ __forceinline__ float at(int j, int i) const
+    {
+        if constexpr (sizeof(T) == 2) return i & 1 ? bf16_hi(w[j][i >> 1]) : bf16_lo(w[j][i >> 1]);
+        else return __uint_as_float(w[j][i]);
+    }
+    __device__ __forceinline__ void load(int j, const T *p)
+    {
+        const uint4 a = load_free((const uint4 *)p);
+        w[j][0] = a.x; w[j][1] = a.y; w[j][2] = a.z; w[j][3] = a.w;
+        if constexpr (sizeof(T) == 4) {
+            const uint4 b = load_free((const uint4 *)p + 1);
+            w[j][4] = b.x; w[j][5] = b.y; w[j][6] = b.z; w[j][7] = b.w;
+        }
+    }
+    __device__ __forceinline__ void load_some(int j, const T *p, int64_t n)      // n entries, which may be none
+    {
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) {
+            if constexpr (sizeof(T) == 2) {
+                const uint32_t lo = 2 * k < n ? (uint32_t)*((const uint16_t *)p + 2 * k) : 0u, hi = 2 * k + 1 < n ? (uint32_t)*((const uint16_t *)p + 2 * k + 1) : 0u;
+                w[j][k] = lo | hi << 16;
+            } else w[j][k] = k < n ? *((const uint32_t *)p + k) : 0u;
+        }
+    }
+    __device__ __forceinline__ void drop(int jh, int ih)                          // 4 x 4 entries become zeros
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int k = 0; k < kWords / 2; ++k) w[jh + j][ih * kWords / 8 + k] = 0u;
+    }
+    // Infinities become NaN, so that they neither enter a scale nor come out as the format's largest value.
+    __device__ __forceinline__ void no_infinity()
+    {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int k = 0; k < kWords; ++k) {
+                if constexpr (sizeof(T) == 2) {
+                    if ((w[j][k] & 0x7FFFu) == 0x7F80u) w[j][k] |= 0x7Fu;
+                    if ((w[j][k] & 0x7FFF0000u) == 0x7F800000u) w[j][k] |= 0x7F0000u;
+                } else if ((w[j][k] & 0x7FFFFFFFu) == 0x7F800000u) w[j][k] |= 0x7FFFFFu;
+            }
+    }
+    // Largest magnitudes of the rows over the 16 lanes that share them (NaN is passed by).
+    __device__ __forceinline__ void row_max(float (&m)[8]) const
+    {
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                uint32_t a[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t x = bf16_max2(w[j + h][0] & 0x7FFF7FFFu, w[j + h][1] & 0x7FFF7FFFu);
+                    x = bf16_max2(x, bf16_max2(w[j + h][2] & 0x7FFF7FFFu, w[j + h][3] & 0x7FFF7FFFu));
+                    a[h] = x;
+                }
+                // (the first row's two halves against the second row's: one word with a row in each half)
+                uint32_t r = bf16_max2(__byte_perm(a[0], a[1], 0x5410), __byte_perm(a[0], a[1], 0x7632));
+#pragma unroll
+                for (int d = 8; d > 0; d >>= 1) r = bf16_max2(r, __shfl_xor_sync(0xFFFFFFFFu, r, d));
+                r = bf16_max2(r, 0u);                              // (rows of nothing but NaN)
+                m[j] = bf16_lo(r); m[j + 1] = bf16_hi(r);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float x = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x = fmaxf(x, fabsf(at(j, i)));
+#pragma unroll
+                for (int d = 8; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, d));
+                m[j] = x;
+            }
+        }
+    }
+    // Largest magnitudes of the columns over the rows of a warp.
+    __device__ __forceinline__ void col_max(float (&m)[8]) const
+    {
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                uint32_t x = 0u;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x = bf16_max2(x, w[j][k] & 0x7FFF7FFFu);
+                x = bf16_max2(x, __shfl_xor_sync(0xFFFFFFFFu, x, 16));
+                m[2 * k] = bf16_lo(x); m[2 * k + 1] = bf16_hi(x);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float x = 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x = fmaxf(x, fabsf(at(j, i)));
+                m[i] = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 16));
+            }
+        }
+    }
+};
+
 template <typename T, bool kE5, bool kWeights>
-__global__ void __launch_bounds__(kQThreads) quantize_f8_kernel(const QParams p)
+__global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 ? 3 : 2) quantize_f8_kernel(const QParams p)
 {
     __shared__ __align__(16) uint8_t s_cols[kF8Block * kF8Block];
-    __shared__ float s_max[8][kF8Block], s_sum[8][kF8Block];
+    __shared__ __align__(16) float s_max[8][kF8Block], s_sum[8][kF8Block];
     __shared__ __align__(16) float s_inv[kF8Block];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, tx = tid & 15, ty = tid >> 4;
     const int64_t ti = (int64_t)blockIdx.x % p.tiles_i, tp = (int64_t)blockIdx.x / p.tiles_i;
     const int64_t c0 = ti * kF8Block + tx * 8, r0 = tp * kF8Block + ty * 8;
     wait_for_previous();
-    const T *X = from_here((const T *)p.X);
+    const T *X = from_here((const T *)p.X) + r0 * p.ldx + c0;
 
-    float v[8][8];
+    QEntries<T> v;
+    if (p.vec && (tp + 1) * kF8Block <= p.P && (ti + 1) * kF8Block <= p.I) {         // (all loads ahead of their first use)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        if (r0 + j < p.P && c0 < p.I) q_load8(X + (r0 + j) * p.ldx, c0, p.I, p.vec, v[j]);
-        else
+        for (int j = 0; j < 8; ++j) v.load(j, X + j * p.ldx);
+    } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[j][i] = 0.f;
+        for (int j = 0; j < 8; ++j) {
+            const int64_t n = r0 + j < p.P ? p.I - c0 : 0;
+            if (p.vec && n >= 8) v.load(j, X + j * p.ldx);
+            else v.load_some(j, X + j * p.ldx, n);
+        }
     }
     if constexpr (kWeights) {
         // a block of Gamma covers whole groups of four rows and of four columns, whatever its shape; dropped weights are zeros, whatever
@@ -78,13 +174,8 @@ __global__ void __launch_bounds__(kQThreads) quantize_f8_kernel(const QParams p)
 #pragma unroll
             for (int jh = 0; jh < 8; jh += 4)
 #pragma unroll
-                for (int ih = 0; ih < 8; ih += 4) {
-                    const bool keep = r0 + jh < p.P && c0 + ih < p.I && load_free(gamma + (r0 + jh) / p.bo * p.NBi + (c0 + ih) / p.bi) != 0u;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) v[jh + j][ih + i] = keep ? v[jh + j][ih + i] : 0.f;
-                }
+                for (int ih = 0; ih < 8; ih += 4)
+                    if (r0 + jh < p.P && c0 + ih < p.I && load_free(gamma + ((r0 + jh) >> p.bo) * p.NBi + ((c0 + ih) >> p.bi)) == 0u) v.drop(jh, ih);
         }
     }
     if (p.partial != nullptr) {
@@ -92,37 +183,19 @@ __global__ void __launch_bounds__(kQThreads) quantize_f8_kernel(const QParams p)
         for (int i = 0; i < 8; ++i) {
             float s = 0.f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s += v[j][i];
+            for (int j = 0; j < 8; ++j) s += v.at(j, i);
             s += __shfl_xor_sync(0xFFFFFFFFu, s, 16);
             if (lane < 16) s_sum[warp][tx * 8 + i] = s;
         }
     }
-
-    // Largest entries of the rows (over the 16 lanes that share them).  fmaxf passes by NaN; an infinity becomes NaN first, so that it neither
-    // enters a scale nor comes out as the format's largest value.
     float rmax[8];
-    auto find_rows = [&]() {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float m = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[j][i]));
-#pragma unroll
-            for (int d = 8; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-            rmax[j] = m;
-        }
-    };
-    find_rows();
+    v.row_max(rmax);
     bool inf = false;
 #pragma unroll
     for (int j = 0; j < 8; ++j) inf |= rmax[j] == __uint_as_float(0x7F800000u);
     if (__any_sync(0xFFFFFFFFu, inf)) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (fabsf(v[j][i]) == __uint_as_float(0x7F800000u)) v[j][i] = __uint_as_float(0x7FFFFFFFu);
-        find_rows();
+        v.no_infinity();
+        v.row_max(rmax);
     }
     if constexpr (kWeights) {
         // one scale for the tile
@@ -138,13 +211,11 @@ __global__ void __launch_bounds__(kQThreads) quantize_f8_kernel(const QParams p)
 #pragma unroll
         for (int j = 0; j < 8; ++j) rmax[j] = m;
     } else if (p.cols != nullptr) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float m = 0.f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(v[j][i]));
-            m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
-            if (lane < 16) s_max[warp][tx * 8 + i] = m;
+        float m[8];
+        v.col_max(m);
+        if (lane < 16) {
+            *(float4 *)&s_max[warp][tx * 8] = make_float4(m[0], m[1], m[2], m[3]);
+            *(float4 *)&s_max[warp][tx * 8 + 4] = make_float4(m[4], m[5], m[6], m[7]);
         }
     }
 
@@ -155,8 +226,8 @@ __global__ void __launch_bounds__(kQThreads) quantize_f8_kernel(const QParams p)
             const uint32_t b = f8_scale_byte<kE5>(__float_as_uint(rmax[j]));
             const float f = f8_inverse(b);
             uint2 w;
-            w.x = f8_pack<kE5>(v[j][0] * f, v[j][1] * f) | f8_pack<kE5>(v[j][2] * f, v[j][3] * f) << 16;
-            w.y = f8_pack<kE5>(v[j][4] * f, v[j][5] * f) | f8_pack<kE5>(v[j][6] * f, v[j][7] * f) << 16;
+            w.x = f8_pack<kE5>(v.at(j, 0) * f, v.at(j, 1) * f) | f8_pack<kE5>(v.at(j, 2) * f, v.at(j, 3) * f) << 16;
+            w.y = f8_pack<kE5>(v.at(j, 4) * f, v.at(j, 5) * f) | f8_pack<kE5>(v.at(j, 6) * f, v.at(j, 7) * f) << 16;
             if (r0 + j < p.P && c0 < p.rows_pitch) *(uint2 *)(p.rows + (r0 + j) * p.rows_pitch + c0) = w;
             if (tx == 0) p.rows_scale[f8_scale_at(r0 + j, ti, p.rows_atoms)] = (uint8_t)b;      // (the scales reach whole groups of 128 rows)
         }
@@ -187,12 +258,15 @@ __global__ void __launch_bounds__(kQThreads) quantize_f8_kernel(const QParams p)
     __syncthreads();
     // transposed form: the eight bytes of a column's rows to shared memory, 8-byte piece ty of column c at place ty ^ (c / 8) so that the
     // lanes of a half warp, eight columns apart, meet different banks
+    float inv[8];
+    *(float4 *)&inv[0] = *(const float4 *)&s_inv[tx * 8];
+    *(float4 *)&inv[4] = *(const float4 *)&s_inv[tx * 8 + 4];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float f = s_inv[tx * 8 + i];
+        const float f = inv[i];
         uint2 w;
-        w.x = f8_pack<kE5>(v[0][i] * f, v[1][i] * f) | f8_pack<kE5>(v[2][i] * f, v[3][i] * f) << 16;
-        w.y = f8_pack<kE5>(v[4][i] * f, v[5][i] * f) | f8_pack<kE5>(v[6][i] * f, v[7][i] * f) << 16;
+        w.x = f8_pack<kE5>(v.at(0, i) * f, v.at(1, i) * f) | f8_pack<kE5>(v.at(2, i) * f, v.at(3, i) * f) << 16;
+        w.y = f8_pack<kE5>(v.at(4, i) * f, v.at(5, i) * f) | f8_pack<kE5>(v.at(6, i) * f, v.at(7, i) * f) << 16;
         *(uint2 *)(s_cols + (tx * 8 + i) * kF8Block + ((ty ^ tx) << 3)) = w;
     }
     __syncthreads();
@@ -326,7 +400,7 @@ bsp_status launch_quantize_f8(const void *X, bsp_dtype xtype, int64_t P, int64_t
     if (rows) { p.rows = (uint8_t *)rows->data; p.rows_scale = (uint8_t *)rows->scale; p.rows_pitch = f8_pitch(I); p.rows_atoms = f8_atoms(I); }
     if (cols) { p.cols = (uint8_t *)cols->data; p.cols_scale = (uint8_t *)cols->scale; p.cols_pitch = f8_pitch(P); p.cols_atoms = f8_atoms(P); }
     if (colsum) p.partial = (float *)((char *)ws + kWsHeader);
-    if (wd) { p.gamma = gamma; p.bo = wd->bo; p.bi = wd->bi; p.NBi = wd->I / wd->bi; }
+    if (wd) { p.gamma = gamma; p.bo = f8_log2(wd->bo); p.bi = f8_log2(wd->bi); p.NBi = wd->I / wd->bi; }
     p.tiles_i = f8_blocks(I);
     const int64_t tiles_p = f8_blocks(P), tiles = p.tiles_i * tiles_p;
     if (tiles > 0x7FFFFFFF) return BSP_ERR_SHAPE;

@@ -350,15 +350,18 @@ __global__ void __launch_bounds__(256) dequantize_f8_kernel(const DParams p)
     const int64_t k0 = tk * kF8Block + tx * 8, r0 = tr * kF8Block + ty * 8;
     wait_for_previous();
     if (k0 >= p.cols || r0 >= p.rows) return;
-    const uint8_t *data = from_here(p.data), *scale = from_here(p.scale);
     const int nk = p.cols - k0 < 8 ? (int)(p.cols - k0) : 8, nr = p.rows - r0 < 8 ? (int)(p.rows - r0) : 8;
+    const uint8_t *data = from_here(p.data) + r0 * p.pitch + k0, *scale = from_here(p.scale) + f8_scale_at(r0, tk, p.atoms);
     uint2 w[8];
+    uint32_t b[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {                       // (the scales of eight rows from a multiple of eight on lie 16 bytes apart)
+        w[j] = j < nr ? load_free((const uint2 *)(data + j * p.pitch)) : make_uint2(0u, 0u);
+        b[j] = load_free(scale + j * 16);
+    }
     float f[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        w[j] = j < nr ? load_free((const uint2 *)(data + (r0 + j) * p.pitch + k0)) : make_uint2(0u, 0u);
-        f[j] = j < nr ? f8_scale(load_free(scale + f8_scale_at(r0 + j, tk, p.atoms))) : 0.f;
-    }
+    for (int j = 0; j < 8; ++j) f[j] = f8_scale(b[j]);
     T *X = (T *)p.X;
     if constexpr (!kTranspose) {
 #pragma unroll
@@ -375,14 +378,14 @@ __global__ void __launch_bounds__(256) dequantize_f8_kernel(const DParams p)
     } else {
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
-            float a[8], b[8];
+            float lo[8], hi[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float2 t = f8_unpack<kE5>((i < 4 ? w[j].x : w[j].y) >> (8 * (i & 2)) & 0xFFFFu);
-                a[j] = t.x * f[j]; b[j] = t.y * f[j];
+                lo[j] = t.x * f[j]; hi[j] = t.y * f[j];
             }
-            if (i < nk) d_store8(X + (k0 + i) * p.ldx + r0, a, nr, p.vec);
-            if (i + 1 < nk) d_store8(X + (k0 + i + 1) * p.ldx + r0, b, nr, p.vec);
+            if (i < nk) d_store8(X + (k0 + i) * p.ldx + r0, lo, nr, p.vec);
+            if (i + 1 < nk) d_store8(X + (k0 + i + 1) * p.ldx + r0, hi, nr, p.vec);
         }
     }
 }

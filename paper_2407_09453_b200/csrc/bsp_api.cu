@@ -363,9 +363,7 @@ bsp_status bsp_linear_f8(const bsp_f8 *w, const void *X, bsp_dtype xtype, int64_
     const bsp_f8 x = {BSP_E4M3, P, w->cols, at, at + align_up(bsp_f8_data_bytes(P, w->cols), 256)};
     rc = check_product(&x, w, bias, Y, ytype, ws);
     if (rc != BSP_OK) return rc;
-    rc = launch_quantize_f8(X, xtype, P, w->cols, ldx, nullptr, nullptr, &x, nullptr, nullptr, ws, (cudaStream_t)stream);
-    if (rc != BSP_OK) return rc;
-    return launch_gemm_f8(x, *w, bias, nullptr, nullptr, Y, ytype, ws, (cudaStream_t)stream);
+    return launch_linear_f8(*w, X, xtype, P, ldx, x, bias, Y, ytype, ws, (cudaStream_t)stream);
 }
 
 bsp_status bsp_check(void *ws, void *stream)

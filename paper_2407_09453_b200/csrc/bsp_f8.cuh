@@ -61,5 +61,7 @@ bsp_status launch_quantize_f8(const void *X, bsp_dtype xtype, int64_t P, int64_t
 bsp_status launch_dequantize_f8(const bsp_f8 &m, void *X, bsp_dtype xtype, int64_t ldx, bool transpose, cudaStream_t st);
 bsp_status launch_gemm_f8(const bsp_f8 &x, const bsp_f8 &w, const float *bias, const bsp_wdesc *wd, const uint8_t *gamma, void *Y, bsp_dtype ytype,
                           void *ws, cudaStream_t st);
+bsp_status launch_linear_f8(const bsp_f8 &w, const void *X, bsp_dtype xtype, int64_t P, int64_t ldx, const bsp_f8 &x, const float *bias, void *Y,
+                            bsp_dtype ytype, void *ws, cudaStream_t st);
 
 }  // namespace bsp

@@ -8,6 +8,7 @@
 // sums in float32: a block of 128 entries is four MMAs with the same scale byte (the instruction names one of the four bytes in
 // a tensor-memory column).  So the scales cost one tcgen05.cp of 512 bytes per 128 rows and 512 entries, and no arithmetic on
 // the accumulators.
+#include <atomic>
 #include <type_traits>
 #include "bsp_f8.cuh"
 #include "bsp_tc.cuh"
@@ -15,33 +16,42 @@
 namespace bsp {
 namespace {
 
-constexpr int kFsThreads = 256;                     // producer warp, MMA warp, two idle warps until the store, four epilogue warps
-constexpr int kFsScaleBytes = 3 * kF8Atom;          // scales of a stage: 128 rows of A, up to 256 rows of B
+constexpr int kFsThreads = 320;                     // producer warp, MMA warp, two groups of four epilogue warps
 constexpr int kFsMaxStages = 8;
 constexpr int kFsSets = 4;                          // scale sets in tensor memory, 16 columns each (A 4, B up to 8)
 constexpr int kFsSmem = 227 * 1024;
+constexpr int kFsChunk = 16;                        // blocks of 128 entries that are summed in the tensor core before float32 registers take over
+constexpr int kFsScales = 2 * kF8Atom;              // scales of a stage: 128 rows of A and of B
 // Shared-memory descriptor of an atom of scales: 32 rows of 16 bytes without swizzle, groups of eight rows 128 bytes apart.
 constexpr uint64_t kFsScaleDesc = (1ull << 16) | (8ull << 32) | (1ull << 46);
 static_assert(kFsMaxStages <= 4 * (kFsSets - 1) + 1, "a set is written again only when the MMAs that read it are done: the ring's barriers see to that");
 
+// ---- small and middle products: a tile of 128 x BN for a CTA, or for a cluster that shares the summed axis ----
+
 struct FsParams {
     CUtensorMap tma, tmb;         // values as bytes, (K, rows), box 128 x 128 and 128 x BN, 128-byte swizzle; zeros past the ends
+    CUtensorMap tmy;              // where `staged`: Y as bytes, (N ey, M), box 128 bytes x 128 rows, 128-byte swizzle
     const uint8_t *sa, *sb;       // scales
     int64_t atoms;                // atoms per 128 rows
     int M, N, BN, n_kb, tiles_n, split, stages, stage_bytes;
+    int off_x, off_recv, off_scales, off_tail;      // offsets in shared memory
     uint32_t idesc;
-    int a_e5, b_e5;
     uint8_t *Y;
-    int bf16, transposed, vec;    // element (m, n) at Y[m N + n], or at Y[n M + m]
+    int bf16, transposed, vec;    // element (m, n) at Y[m N + n], or at Y[n M + m]; rows that can be written 16 bytes at a time
+    int staged;                   // the output leaves by TMA stores
     const float *bias;
     const uint8_t *gamma;
-    int bo, bi, NBi;
+    int bo, bi, NBi;              // Gamma's blocks: logarithms of their sizes, blocks in a row
+    const void *X;                // kX: the rows of B before they are quantised, ldx entries apart
+    int64_t ldx, K;
+    int xvec;                     // rows of X can be read four entries at a time
     int *status;
 };
 
 struct FsTail {
-    uint64_t full[kFsMaxStages], empty[kFsMaxStages], acc;
+    uint64_t full[kFsMaxStages], empty[kFsMaxStages], acc_full[2], acc_free[2], x_ready;
     uint32_t tmem, fail;
+    float bias[128];
 };
 
 // 16 consecutive accumulator columns of this thread's tensor-memory lane.
@@ -56,39 +66,69 @@ __device__ __forceinline__ void fs_load16(uint32_t taddr, uint32_t (&v)[16])
                    "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]) :: "memory");
 }
 
-// Four partial sums of this CTA's tile or of the same tile in another CTA of the cluster.
-__device__ __forceinline__ float4 fs_peer4(uint32_t addr, uint32_t rank)
+// Four entries of a row of X, `n` of which exist.
+__device__ __forceinline__ void fs_load_x(const float *x, int64_t n, int vec, float (&v)[4])
 {
-    float4 v;
-    asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %4, %5;\n ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [a];\n}\n"
-                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr), "r"(rank) : "memory");
-    return v;
+    if (vec && n >= 4) {
+        const float4 a = load_free((const float4 *)x);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    } else
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = i < n ? __uint_as_float(load_free((const uint32_t *)x + i)) : 0.f;
+}
+__device__ __forceinline__ void fs_load_x(const __nv_bfloat16 *x, int64_t n, int vec, float (&v)[4])
+{
+    if (vec && n >= 4) {
+        const uint2 a = load_free((const uint2 *)x);
+        v[0] = __uint_as_float(a.x << 16); v[1] = __uint_as_float(a.x & 0xFFFF0000u);
+        v[2] = __uint_as_float(a.y << 16); v[3] = __uint_as_float(a.y & 0xFFFF0000u);
+    } else
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = i < n ? __bfloat162float(x[i]) : 0.f;
 }
 
-// One tile of 128 x BN per cluster; CTA r of the cluster sums its share of the blocks, and the shares are added up in the order of the
-// ranks through distributed shared memory.
-__global__ void __launch_bounds__(kFsThreads, 1) gemm_f8_kernel(const __grid_constant__ FsParams p)
+// What an element becomes, two neighbours of a row at a time.
+__device__ __forceinline__ uint32_t fs_pack(float lo, float hi)
 {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *(const uint32_t *)&h;
+}
+
+// One tile of 128 x BN per cluster.  CTA r of the cluster sums its share of the blocks, sends the columns that CTA s stores to s through
+// distributed shared memory, and s adds the shares up in the order of the ranks: every CTA stores BN / split columns of the tile.
+// (A cluster of eight finds room for 15 of its kind on the 148 SMs, of four for 33, of two for 74.)
+// Chunks of kFsChunk blocks go to two accumulators in turn and are added up in registers (256 instructions in a row into one
+// accumulator, 8192 entries, were off by 1.9e-6 of the result, chunks by 5.5e-7; plain float32 sums by 4.2e-7).
+// T: type of X where its rows are quantised here (rows of B, e4m3), void where B comes as an 8-bit matrix.
+template <typename T>
+__global__ void __launch_bounds__(kFsThreads, 1) gemm_f8_tile_kernel(const __grid_constant__ FsParams p)
+{
+    constexpr bool kX = !std::is_same_v<T, void>;
     extern __shared__ __align__(1024) uint8_t smem[];
-    FsTail &tail = *(FsTail *)(smem + (size_t)p.stages * (p.stage_bytes + kFsScaleBytes));
+    FsTail &tail = *(FsTail *)(smem + p.off_tail);
     volatile uint32_t &s_fail = tail.fail;
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
     const int S = p.stages, split = p.split, tile = (int)blockIdx.x / split, rank = (int)blockIdx.x - tile * split;
     const int tm = tile / p.tiles_n, tn = tile - tm * p.tiles_n, m0 = tm * 128, n0 = tn * p.BN, BN = p.BN;
     const int kb0 = (int)((long long)p.n_kb * rank / split), kb1 = (int)((long long)p.n_kb * (rank + 1) / split);
-    const uint32_t ring = sm32(smem), scales = ring + (uint32_t)(S * p.stage_bytes);
-    const uint32_t cols = BN + 64 <= 128 ? 128u : BN + 64 <= 256 ? 256u : 512u;
+    const uint32_t ring = sm32(smem), scales = ring + (uint32_t)p.off_scales, xs = ring + (uint32_t)p.off_x;
+    const uint32_t xs_scales = xs + (uint32_t)((kb1 - kb0) * BN * 128);      // (kX)
+    const uint32_t cols = BN <= 32 ? 128u : BN <= 64 ? 256u : 512u;          // two accumulators and 64 columns of scales
 
     if (tid == 0) {
         for (int s = 0; s < S; ++s) {
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(sm32(&tail.full[s])), "r"(1) : "memory");
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(sm32(&tail.empty[s])), "r"(1) : "memory");
         }
-        asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(sm32(&tail.acc)), "r"(1) : "memory");
+        for (int b = 0; b < 2; ++b) {
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(sm32(&tail.acc_full[b])), "r"(1) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(sm32(&tail.acc_free[b])), "r"(8) : "memory");
+        }
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(sm32(&tail.x_ready)), "r"(8) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         s_fail = (ring & 1023u) == 0u ? 0u : 2u;
         asm volatile("prefetch.tensormap [%0];\n" ::"l"(&p.tma) : "memory");
-        asm volatile("prefetch.tensormap [%0];\n" ::"l"(&p.tmb) : "memory");
+        if constexpr (!kX) asm volatile("prefetch.tensormap [%0];\n" ::"l"(&p.tmb) : "memory");
     }
     if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(sm32(&tail.tmem)), "r"(cols) : "memory");
@@ -100,32 +140,39 @@ __global__ void __launch_bounds__(kFsThreads, 1) gemm_f8_kernel(const __grid_con
     asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+    // (the CTAs of a cluster run once this barrier is complete: what they send each other waits for it)
+    if (split > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;\n" ::: "memory");
     const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, tail.tmem, 0), sf = tmem + cols - 64u;
     const bool run = __shfl_sync(0xFFFFFFFFu, s_fail, 0) == 0u;
     const uint32_t full0 = sm32(&tail.full[0]), empty0 = sm32(&tail.empty[0]);
-    // atoms of B's scales: those of the tile's rows, of which the second may not exist
-    const int at_b = n0 >> 7, two = BN > 128 && n0 + 128 < p.N ? 1 : 0;
 
+    float acc[4][16];                                 // (epilogue warps)
     if (warp == 0) {
         // ================= producer =================
         if (run) {
-            const uint8_t *sa = p.sa + (int64_t)tm * p.atoms * kF8Atom, *sb = p.sb + (int64_t)at_b * p.atoms * kF8Atom, *sb2 = sb + p.atoms * kF8Atom;
+            const uint8_t *sa = p.sa + (int64_t)tm * p.atoms * kF8Atom, *sb = p.sb + (int64_t)(n0 >> 7) * p.atoms * kF8Atom;
             uint32_t slot = 0, par = 1, issued = 0;
             bool ok = true;
             for (int kb = kb0; kb < kb1; ++kb) {
                 if (!__all_sync(0xFFFFFFFFu, gt_poll(empty0 + slot * 8u, par)) || s_fail) { ok = false; break; }
-                const uint32_t with_scales = kb == kb0 || (kb & 3) == 0 ? 1u : 0u, dst = ring + slot * (uint32_t)p.stage_bytes, sdst = scales + slot * kFsScaleBytes;
-                const uint32_t bytes = (uint32_t)p.stage_bytes + with_scales * (uint32_t)((2 + two) * kF8Atom);
+                const uint32_t with = kb == kb0 || (kb & 3) == 0 ? 1u : 0u, dst = ring + slot * (uint32_t)p.stage_bytes, sdst = scales + slot * kFsScales;
+                const uint32_t bytes = (uint32_t)p.stage_bytes + with * (kX ? kF8Atom : 2 * kF8Atom);
                 const int64_t at = (int64_t)(kb >> 2) * kF8Atom;
-                asm volatile("{\n .reg .pred e, s, t;\n elect.sync _|e, 0xFFFFFFFF;\n setp.ne.b32 s, %9, 0;\n and.pred s, s, e;\n setp.ne.b32 t, %10, 0;\n and.pred t, t, s;\n"
-                             " @e mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n"
-                             " @e cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%2], [%3, {%4, %5}], [%0];\n"
-                             " @e cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%6], [%7, {%4, %8}], [%0];\n"
-                             " @s cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%11], [%12], 512, [%0];\n"
-                             " @s cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%13], [%14], 512, [%0];\n"
-                             " @t cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%15], [%16], 512, [%0];\n}\n"
-                             ::"r"(full0 + slot * 8u), "r"(bytes), "r"(dst), "l"(&p.tma), "r"(kb * 128), "r"(m0), "r"(dst + 16384u), "l"(&p.tmb), "r"(n0),
-                               "r"(with_scales), "r"(two), "r"(sdst), "l"(sa + at), "r"(sdst + 512u), "l"(sb + at), "r"(sdst + 1024u), "l"(sb2 + at) : "memory");
+                if constexpr (kX)
+                    asm volatile("{\n .reg .pred e, s;\n elect.sync _|e, 0xFFFFFFFF;\n setp.ne.b32 s, %6, 0;\n and.pred s, s, e;\n"
+                                 " @e mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n"
+                                 " @s cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%7], [%8], 512, [%0];\n"
+                                 " @e cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%2], [%3, {%4, %5}], [%0];\n}\n"
+                                 ::"r"(full0 + slot * 8u), "r"(bytes), "r"(dst), "l"(&p.tma), "r"(kb * 128), "r"(m0), "r"(with), "r"(sdst), "l"(sa + at) : "memory");
+                else
+                    asm volatile("{\n .reg .pred e, s;\n elect.sync _|e, 0xFFFFFFFF;\n setp.ne.b32 s, %9, 0;\n and.pred s, s, e;\n"
+                                 " @e mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n"
+                                 " @s cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%10], [%11], 512, [%0];\n"
+                                 " @s cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%12], [%13], 512, [%0];\n"
+                                 " @e cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%2], [%3, {%4, %5}], [%0];\n"
+                                 " @e cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%6], [%7, {%4, %8}], [%0];\n}\n"
+                                 ::"r"(full0 + slot * 8u), "r"(bytes), "r"(dst), "l"(&p.tma), "r"(kb * 128), "r"(m0), "r"(dst + 16384u), "l"(&p.tmb), "r"(n0),
+                                   "r"(with), "r"(sdst), "l"(sa + at), "r"(sdst + kF8Atom), "l"(sb + at) : "memory");
                 ++issued;
                 if (++slot == (uint32_t)S) { slot = 0; par ^= 1u; }
             }
@@ -141,118 +188,268 @@ __global__ void __launch_bounds__(kFsThreads, 1) gemm_f8_kernel(const __grid_con
     } else if (warp == 1) {
         // ================= MMA issuer =================
         if (run) {
-            uint32_t slot = 0, par = 0, set = 0, acc = 0;
+            uint32_t slot = 0, par = 0, set = 0, chunk = 0;
             bool ok = true;
-            for (int kb = kb0; kb < kb1; ++kb) {
+            if constexpr (kX) ok = gt_poll_stage(sm32(&tail.x_ready), 0u);
+            for (int kb = kb0; kb < kb1 && ok; ++kb) {
+                const bool fresh = (kb - kb0) % kFsChunk == 0;
+                if (fresh && chunk >= 2u && !gt_poll_stage(sm32(&tail.acc_free[chunk & 1u]), ((chunk >> 1) & 1u) ^ 1u)) { ok = false; break; }
                 if (!gt_poll_stage(full0 + slot * 8u, par)) { ok = false; break; }
-                const uint32_t with_scales = kb == kb0 || (kb & 3) == 0 ? 1u : 0u;
-                if (with_scales && kb != kb0) set = set + 1u == kFsSets ? 0u : set + 1u;
-                const uint32_t a16 = (ring + slot * (uint32_t)p.stage_bytes) >> 4, s16 = (scales + slot * kFsScaleBytes) >> 4;
-                const uint64_t da = kGtDesc | (uint64_t)(a16 & 0x3FFFu), db = kGtDesc | (uint64_t)((a16 + 1024u) & 0x3FFFu);
-                const uint64_t ds = kFsScaleDesc | (uint64_t)(s16 & 0x3FFFu);
-                const uint32_t fa = sf + set * 16u, fb = fa + 8u, id = (uint32_t)kb & 3u;
-                const uint32_t idesc = p.idesc | (id << 4) | (id << 29);
-                asm volatile("{\n .reg .pred e, s, t, p, q;\n .reg .b64 a1, a2, a3, b1, b2, b3, s1, s2;\n .reg .b32 f2;\n"
-                             " elect.sync _|e, 0xFFFFFFFF;\n setp.ne.b32 s, %8, 0;\n and.pred s, s, e;\n setp.ne.b32 t, %9, 0;\n and.pred t, t, s;\n"
-                             " setp.ne.b32 p, %10, 0;\n setp.eq.b32 q, %10, %10;\n"
-                             " add.u64 s1, %4, 32;\n add.u64 s2, %4, 64;\n add.u32 f2, %6, 4;\n"
-                             " @s tcgen05.cp.cta_group::1.32x128b.warpx4 [%5], %4;\n"
-                             " @s tcgen05.cp.cta_group::1.32x128b.warpx4 [%6], s1;\n"
-                             " @t tcgen05.cp.cta_group::1.32x128b.warpx4 [f2], s2;\n"
+                const uint32_t with = kb == kb0 || (kb & 3) == 0 ? 1u : 0u;
+                if (with && kb != kb0) set = (set + 1u) & (kFsSets - 1u);
+                const uint32_t a16 = (ring + slot * (uint32_t)p.stage_bytes) >> 4, s16 = (scales + slot * kFsScales) >> 4;
+                const uint32_t b16 = kX ? (xs + (uint32_t)((kb - kb0) * BN * 128)) >> 4 : a16 + 1024u;
+                const uint32_t t16 = kX ? (xs_scales + (uint32_t)((kb >> 2) - (kb0 >> 2)) * kF8Atom) >> 4 : s16 + (kF8Atom >> 4);
+                const uint64_t da = kGtDesc | (uint64_t)(a16 & 0x3FFFu), db = kGtDesc | (uint64_t)(b16 & 0x3FFFu);
+                const uint64_t ds = kFsScaleDesc | (uint64_t)(s16 & 0x3FFFu), dt = kFsScaleDesc | (uint64_t)(t16 & 0x3FFFu);
+                // A tile of 32 or 64 rows of B that starts inside an atom: its columns of scales move to the front, as an MMA takes scales from a
+                // multiple of four columns on (any other address is a misaligned one).
+                const uint32_t skip = (uint32_t)(n0 & 127) >> 5;
+                if (with && skip) {
+                    const uint32_t at = (t16 << 4) + (uint32_t)lane * 16u;
+                    uint32_t w[4];
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
+                    const uint32_t lo = skip == 1u ? w[1] : skip == 2u ? w[2] : w[3], hi = skip == 1u ? w[2] : w[3];
+                    asm volatile("st.shared.v2.b32 [%0], {%1, %2};\n fence.proxy.async.shared::cta;\n" ::"r"(at), "r"(lo), "r"(hi) : "memory");
+                    __syncwarp();
+                }
+                const uint32_t fa = sf + set * 16u, fb = fa + 8u, id = (uint32_t)kb & 3u, idesc = p.idesc | (id << 4) | (id << 29);
+                asm volatile("{\n .reg .pred e, s, p, q;\n .reg .b64 a1, a2, a3, b1, b2, b3;\n"
+                             " elect.sync _|e, 0xFFFFFFFF;\n setp.ne.b32 s, %9, 0;\n and.pred s, s, e;\n setp.ne.b32 p, %10, 0;\n setp.eq.b32 q, %10, %10;\n"
+                             " @s tcgen05.cp.cta_group::1.32x128b.warpx4 [%6], %4;\n"
+                             " @s tcgen05.cp.cta_group::1.32x128b.warpx4 [%7], %5;\n"
                              " add.u64 a1, %1, 2;\n add.u64 a2, %1, 4;\n add.u64 a3, %1, 6;\n"
                              " add.u64 b1, %2, 2;\n add.u64 b2, %2, 4;\n add.u64 b3, %2, 6;\n"
-                             " @e tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%5], [%6], p;\n"
-                             " @e tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a1, b1, %3, [%5], [%6], q;\n"
-                             " @e tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a2, b2, %3, [%5], [%6], q;\n"
-                             " @e tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a3, b3, %3, [%5], [%6], q;\n"
-                             " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%7];\n}\n"
-                             ::"r"(tmem), "l"(da), "l"(db), "r"(idesc), "l"(ds), "r"(fa), "r"(fb), "r"(empty0 + slot * 8u), "r"(with_scales), "r"(two), "r"(acc)
-                             : "memory");
-                acc = 1u;
+                             " @e tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%6], [%7], p;\n"
+                             " @e tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a1, b1, %3, [%6], [%7], q;\n"
+                             " @e tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a2, b2, %3, [%6], [%7], q;\n"
+                             " @e tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a3, b3, %3, [%6], [%7], q;\n"
+                             " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%8];\n}\n"
+                             ::"r"(tmem + (chunk & 1u) * (uint32_t)BN), "l"(da), "l"(db), "r"(idesc), "l"(ds), "l"(dt), "r"(fa), "r"(fb), "r"(empty0 + slot * 8u), "r"(with),
+                               "r"(fresh ? 0u : 1u) : "memory");
                 if (++slot == (uint32_t)S) { slot = 0; par ^= 1u; }
+                if (kb + 1 == kb1 || (kb + 1 - kb0) % kFsChunk == 0) {
+                    gt_commit_elected<false>(sm32(&tail.acc_full[chunk & 1u]));
+                    ++chunk;
+                }
             }
-            if (ok) gt_commit_elected<false>(sm32(&tail.acc));
-            else if (lane == 0) atomicExch(&tail.fail, 1u);
+            if (!ok && lane == 0) atomicExch(&tail.fail, 1u);
         }
-    } else if (warp >= 4) {
-        // ================= accumulators to shared memory =================
-        // (All MMAs are done, so the ring is free.)  Rows of n for an output whose rows are n, pitch BN + 4 words; rows of m otherwise.
-        if (run) {
-            if (!__all_sync(0xFFFFFFFFu, gt_wait(sm32(&tail.acc), 0u))) { if (lane == 0) atomicExch(&tail.fail, 1u); }
-            else {
-                asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-                const int q = warp & 3, m = q * 32 + lane;
-                float *part = (float *)smem;
-                for (int c = 0; c < BN; c += 16) {
-                    uint32_t v[16];
-                    fs_load16(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)c, v);
-                    if (p.transposed) {
+    } else if (run) {
+        const int w = warp - 2, q = warp & 3, grp = w >> 2;
+        if constexpr (kX) {
+            // ================= rows of X to 8 bits: a warp takes 128 entries of a row, four to a lane =================
+            const T *X = from_here((const T *)p.X);
+            const int rows = p.N < BN ? p.N : BN, items = (kb1 - kb0) * rows;
+            constexpr int kBatch = 4;
+            for (int i0 = w; i0 < items; i0 += 8 * kBatch) {
+                float v[kBatch][4], m[kBatch];
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) part[(c + e) * 128 + m] = __uint_as_float(v[e]);
-                    } else {
+                for (int u = 0; u < kBatch; ++u) {
+                    const int i = i0 + 8 * u, b = i / rows, r = i - b * rows;
+                    const int64_t c = (int64_t)(kb0 + b) * kF8Block + lane * 4;
+                    fs_load_x(X + r * p.ldx + c, i < items ? p.K - c : 0, p.xvec, v[u]);
+                }
 #pragma unroll
-                        for (int e = 0; e < 16; e += 4) *(uint4 *)(part + m * (BN + 4) + c + e) = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+                for (int u = 0; u < kBatch; ++u) m[u] = fmaxf(fmaxf(fabsf(v[u][0]), fabsf(v[u][1])), fmaxf(fabsf(v[u][2]), fabsf(v[u][3])));
+#pragma unroll
+                for (int d = 16; d > 0; d >>= 1)
+#pragma unroll
+                    for (int u = 0; u < kBatch; ++u) m[u] = fmaxf(m[u], __shfl_xor_sync(0xFFFFFFFFu, m[u], d));
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) {
+                    const int i = i0 + 8 * u, b = i / rows, r = i - b * rows;
+                    if (m[u] == __uint_as_float(0x7F800000u)) {        // (infinities become NaN and enter no scale)
+                        m[u] = 0.f;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            if (fabsf(v[u][e]) == __uint_as_float(0x7F800000u)) v[u][e] = __uint_as_float(0x7FFFFFFFu);
+                            m[u] = fmaxf(m[u], fabsf(v[u][e]));
+                        }
+#pragma unroll
+                        for (int d = 16; d > 0; d >>= 1) m[u] = fmaxf(m[u], __shfl_xor_sync(0xFFFFFFFFu, m[u], d));
+                    }
+                    const uint32_t byte = f8_scale_byte<false>(__float_as_uint(m[u]));
+                    const float f = f8_inverse(byte);
+                    if (i < items) {
+                        const uint32_t word = f8_pack<false>(v[u][0] * f, v[u][1] * f) | f8_pack<false>(v[u][2] * f, v[u][3] * f) << 16;
+                        const uint32_t row = xs + (uint32_t)(b * BN * 128 + r * 128);
+                        asm volatile("st.shared.b32 [%0], %1;\n" ::"r"(row + ((((uint32_t)lane >> 2) ^ ((uint32_t)r & 7u)) << 4) + ((uint32_t)lane & 3u) * 4u), "r"(word) : "memory");
+                        if (lane == 0)
+                            asm volatile("st.shared.u8 [%0], %1;\n" ::"r"(xs_scales + (uint32_t)(((kb0 + b) >> 2) - (kb0 >> 2)) * kF8Atom +
+                                                                         (uint32_t)((r & 31) * 16 + (r >> 5) * 4 + ((kb0 + b) & 3))), "r"(byte) : "memory");
                     }
                 }
+            }
+            asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+            __syncwarp();
+            if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(sm32(&tail.x_ready)) : "memory");
+        }
+        // ================= sums: group g takes the columns BN / 2 g .. (all 16 where there are no more) =================
+        const float *bias = from_here(p.bias);
+        if (tid - 64 < 128) {
+            const int at = tid - 64, i = p.transposed ? m0 + at : n0 + at;
+            tail.bias[at] = bias != nullptr && i < (p.transposed ? p.M : p.N) && (p.transposed || at < BN) ? __uint_as_float(load_free((const uint32_t *)bias + i)) : 0.f;
+        }
+        const int pieces = BN >= 32 ? BN / 32 : 1 - grp;
+        const int chunks = (kb1 - kb0 + kFsChunk - 1) / kFsChunk;
+        for (int c = 0; c < chunks; ++c) {
+            const uint32_t buf = (uint32_t)c & 1u;
+            if (!__all_sync(0xFFFFFFFFu, gt_wait(sm32(&tail.acc_full[buf]), ((uint32_t)c >> 1) & 1u) && s_fail == 0u)) { if (lane == 0) atomicExch(&tail.fail, 1u); break; }
+            asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+            const uint32_t t = tmem + ((uint32_t)(q * 32) << 16) + buf * (uint32_t)BN + (uint32_t)(grp * (BN / 2));
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k < pieces) {
+                    uint32_t v[16];
+                    fs_load16(t + (uint32_t)k * 16u, v);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[k][e] = c == 0 ? __uint_as_float(v[e]) : acc[k][e] + __uint_as_float(v[e]);
+                }
+            asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+            __syncwarp();
+            if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(sm32(&tail.acc_free[buf])) : "memory");
+        }
+    }
+    // ================= the shares to the CTAs that store them =================
+    __syncwarp();
+    const int valid_n = p.N - n0 < BN ? p.N - n0 : BN, per = BN / split, row = (warp & 3) * 32 + lane, grp = (warp - 2) >> 2;
+    const int first = grp * (BN / 2), pieces = BN >= 32 ? BN / 32 : 1 - grp;
+    const bool epilogue = warp >= 2;
+    if (split > 1) {
+        asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+        if (epilogue && run) {
+            // at the receiver: [rank of the sender][its column][128 rows]
+            const uint32_t mine = ring + (uint32_t)p.off_recv + (uint32_t)(rank * per * 128 + row) * 4u;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k < pieces)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int c = first + k * 16 + e, to = c / per;
+                        if (c < valid_n)
+                            asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %0, %1;\n st.shared::cluster.f32 [a], %2;\n}\n"
+                                         ::"r"(mine + (uint32_t)(c - to * per) * 512u), "r"(to), "f"(acc[k][e]) : "memory");
+                    }
+        }
+        asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+    } else __syncthreads();
+    // (whoever gave up did so before the barrier: all warps see the same)
+    const bool fine = run && s_fail == 0u;
+    const uint8_t *gamma = from_here(p.gamma);
+    const int ey = p.bf16 ? 2 : 4;
+    if (!epilogue || !fine) {
+    } else if (split > 1) {
+        const int c0 = rank * per, n = valid_n - c0 < per ? valid_n - c0 : per;        // columns of this CTA's share
+        const float *recv = (const float *)(smem + p.off_recv);
+        const int m = (tid - 64) & 127, half = (tid - 64) >> 7;
+        auto sum = [&](int c) {
+            float v = recv[c * 128 + m];
+            for (int s = 1; s < split; ++s) v += recv[(s * per + c) * 128 + m];
+            return v;
+        };
+        if (m0 + m < p.M) {
+            if (p.transposed)
+                for (int c = half; c < n; c += 2) {
+                    const float v = sum(c) + tail.bias[m];
+                    const int64_t at = (int64_t)(n0 + c0 + c) * p.M + m0 + m;
+                    if (p.bf16) ((__nv_bfloat16 *)p.Y)[at] = __float2bfloat16_rn(v);
+                    else ((float *)p.Y)[at] = v;
+                }
+            else
+                for (int c = half * 4; c < n; c += 8) {
+                    float v[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = c + e < n ? sum(c + e) + tail.bias[c0 + c + e] : 0.f;
+                    const int col = n0 + c0 + c;
+                    if (gamma != nullptr && load_free(gamma + (int64_t)((m0 + m) >> p.bo) * p.NBi + (col >> p.bi)) == 0u) v[0] = v[1] = v[2] = v[3] = 0.f;
+                    const int64_t at = (int64_t)(m0 + m) * p.N + col;
+                    if (p.vec && c + 4 <= n) {
+                        if (p.bf16) *(uint2 *)((__nv_bfloat16 *)p.Y + at) = make_uint2(fs_pack(v[0], v[1]), fs_pack(v[2], v[3]));
+                        else *(float4 *)((float *)p.Y + at) = make_float4(v[0], v[1], v[2], v[3]);
+                    } else
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (c + e < n) {
+                                if (p.bf16) ((__nv_bfloat16 *)p.Y)[at + e] = __float2bfloat16_rn(v[e]);
+                                else ((float *)p.Y)[at + e] = v[e];
+                            }
+                }
+        }
+    } else {
+        const int m = m0 + row;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (k < pieces) {
+                const int c0 = first + k * 16;
+                if (p.transposed) {
+                    if (m < p.M)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (c0 + e < valid_n) {
+                                const float v = acc[k][e] + tail.bias[row];
+                                const int64_t at = (int64_t)(n0 + c0 + e) * p.M + m;
+                                if (p.bf16) ((__nv_bfloat16 *)p.Y)[at] = __float2bfloat16_rn(v);
+                                else ((float *)p.Y)[at] = v;
+                            }
+                    continue;
+                }
+                float v[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[e] = acc[k][e] + tail.bias[c0 + e];
+                if (gamma != nullptr && m < p.M) {
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4)
+                        if (c0 + e < valid_n && load_free(gamma + (int64_t)(m >> p.bo) * p.NBi + ((n0 + c0 + e) >> p.bi)) == 0u) v[e] = v[e + 1] = v[e + 2] = v[e + 3] = 0.f;
+                }
+                if (p.staged) {
+                    // to the ring, which is free: slabs of 128 bytes of every row under the swizzle of the stores
+                    const uint32_t byte = (uint32_t)(c0 * ey), slab = ring + (byte >> 7) * 16384u + (uint32_t)row * 128u, piece = (byte & 127u) >> 4, sw = (uint32_t)row & 7u;
+                    if (p.bf16) {
+#pragma unroll
+                        for (uint32_t j = 0; j < 2u; ++j)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(slab + (((piece + j) ^ sw) << 4)), "r"(fs_pack(v[8 * j], v[8 * j + 1])),
+                                         "r"(fs_pack(v[8 * j + 2], v[8 * j + 3])), "r"(fs_pack(v[8 * j + 4], v[8 * j + 5])), "r"(fs_pack(v[8 * j + 6], v[8 * j + 7])) : "memory");
+                    } else {
+#pragma unroll
+                        for (uint32_t j = 0; j < 4u; ++j)
+                            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};\n" ::"r"(slab + (((piece + j) ^ sw) << 4)), "f"(v[4 * j]), "f"(v[4 * j + 1]), "f"(v[4 * j + 2]),
+                                         "f"(v[4 * j + 3]) : "memory");
+                    }
+                } else if (m < p.M) {
+                    const int64_t at = (int64_t)m * p.N + n0 + c0;
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        if (p.vec && c0 + e + 4 <= valid_n) {
+                            if (p.bf16) *(uint2 *)((__nv_bfloat16 *)p.Y + at + e) = make_uint2(fs_pack(v[e], v[e + 1]), fs_pack(v[e + 2], v[e + 3]));
+                            else *(float4 *)((float *)p.Y + at + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+                        } else
+#pragma unroll
+                            for (int f = 0; f < 4; ++f)
+                                if (c0 + e + f < valid_n) {
+                                    if (p.bf16) ((__nv_bfloat16 *)p.Y)[at + e + f] = __float2bfloat16_rn(v[e + f]);
+                                    else ((float *)p.Y)[at + e + f] = v[e + f];
+                                }
+                    }
+                }
+            }
+        if (p.staged) {
+            asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+            asm volatile("bar.sync 1, 256;\n" ::: "memory");
+            if (tid == 64) {
+                for (int b = 0; b * 128 < BN * ey; ++b)
+                    if (n0 + b * 128 / ey < p.N)
+                        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];\n"
+                                     ::"l"(&p.tmy), "r"(ring + (uint32_t)b * 16384u), "r"(n0 * ey + b * 128), "r"(m0) : "memory");
+                asm volatile("cp.async.bulk.commit_group;\n cp.async.bulk.wait_group.read 0;\n" ::: "memory");
             }
         }
     }
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
-    if (split > 1) gt_sync_all<true>(); else __syncthreads();
-    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(cols) : "memory");
-
-    // ================= the shares added up, bias, Gamma, output =================
-    // CTA r stores the r-th part of the tile's pieces of four.
-    if (run && s_fail == 0u) {
-        const int rows = p.transposed ? (p.N - n0 < BN ? p.N - n0 : BN) : (p.M - m0 < 128 ? p.M - m0 : 128);
-        const int per_row = p.transposed ? 32 : BN / 4, pitch = p.transposed ? 128 : BN + 4;
-        const int lead0 = p.transposed ? n0 : m0, in0 = p.transposed ? m0 : n0, in_end = p.transposed ? p.M : p.N;
-        const int units = rows * per_row, u0 = (int)((long long)units * rank / split), u1 = (int)((long long)units * (rank + 1) / split);
-        const float *bias = from_here(p.bias);
-        const uint8_t *gamma = from_here(p.gamma);
-        for (int u = u0 + tid; u < u1; u += kFsThreads) {
-            const int r = u / per_row, c = (u - r * per_row) * 4, in = in0 + c;
-            if (in >= in_end) continue;
-            const uint32_t at = ring + (uint32_t)(r * pitch + c) * 4u;
-            float4 v;
-            if (split == 1) v = *(const float4 *)(smem + (at - ring));
-            else {
-                v = fs_peer4(at, 0u);
-                for (int s = 1; s < split; ++s) {
-                    const float4 w = fs_peer4(at, (uint32_t)s);
-                    v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
-                }
-            }
-            const int left = in_end - in;
-            if (bias != nullptr) {
-                float b[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) b[e] = e < left ? __uint_as_float(load_free((const uint32_t *)bias + in + e)) : 0.f;
-                v.x += b[0]; v.y += b[1]; v.z += b[2]; v.w += b[3];
-            }
-            if (gamma != nullptr && load_free(gamma + (int64_t)((lead0 + r) / p.bo) * p.NBi + in / p.bi) == 0u) v = make_float4(0.f, 0.f, 0.f, 0.f);
-            const int64_t out = (int64_t)(lead0 + r) * in_end + in;
-            const float x[4] = {v.x, v.y, v.z, v.w};
-            if (p.bf16) {
-                __nv_bfloat16 *y = (__nv_bfloat16 *)p.Y + out;
-                if (p.vec) {
-                    const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
-                    *(uint2 *)y = make_uint2(*(const uint32_t *)&a, *(const uint32_t *)&b);
-                } else
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) if (e < left) y[e] = __float2bfloat16_rn(x[e]);
-            } else {
-                float *y = (float *)p.Y + out;
-                if (p.vec) *(float4 *)y = v;
-                else
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) if (e < left) y[e] = x[e];
-            }
-        }
-    }
-    if (split > 1) gt_sync_all<true>();           // (no CTA leaves while another reads its memory)
+    __syncthreads();
     if (s_fail == 1u && tid == 0) atomicMax(p.status, (int)BSP_ERR_TIMEOUT);
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(cols) : "memory");
 }
 
 // ---- large products: persistent pairs of CTAs ----
@@ -262,9 +459,9 @@ constexpr int kFpThreads = 384;                     // producer warp, MMA warp, 
 constexpr int kFpFew = 40, kFpMany = 232;
 constexpr int kFpStage = 32768;                     // 128 rows of A and 128 rows (half of the tile's) of B
 constexpr int kFpStages = 5;
+constexpr int kFpScales = 3 * kF8Atom;          // scales of a stage: 128 rows of A, 256 rows of B
 constexpr int kFpStaging = 16384;                   // of a group: 128 rows of 128 bytes
 constexpr int kFpSecond = 192;                      // first column of the second accumulator: the last 64 of the first lie under it
-constexpr int kFpChunk = 16;                        // blocks of 128 entries that are summed in the tensor core before float32 registers take over
 
 struct FpParams {
     CUtensorMap tma, tmb;         // values as bytes, (K, rows), box 128 x 128, 128-byte swizzle
@@ -283,19 +480,18 @@ struct FpTail {
     uint32_t tmem, fail;
     __align__(16) float bias[2][128];
 };
-constexpr int kFpSmem = kFpStages * (kFpStage + kFsScaleBytes) + 2 * kFpStaging + (int)sizeof(FpTail);
+constexpr int kFpSmem = kFpStages * (kFpStage + kFpScales) + 2 * kFpStaging + (int)sizeof(FpTail);
 static_assert(kFpSmem <= kFsSmem, "shared memory of a CTA");
 
 // A pair of CTAs owns tiles of 256 x 256: CTA r of the pair the rows 128 r .. of the tile, and loads these and its half of the tile's rows
 // of B; the leader issues MMAs of 256 x 256 x 32 for both.  Two accumulators of 256 columns that overlap by 64, whose columns the
 // epilogue reads first, leave 64 columns for the scales: the next tile's MMAs start when these 64 have been read.
-// kF32: sums of kFpChunk blocks in the tensor core, of these in registers (256 instructions in a row, 8192 entries, were off by 1.9e-6 of
-// the result, 64 by ...).
+// kF32: chunks of kFsChunk blocks are summed in the tensor core, these in registers (as above).
 template <bool kF32>
 __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __grid_constant__ FpParams p)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
-    FpTail &tail = *(FpTail *)(smem + kFpStages * (kFpStage + kFsScaleBytes) + 2 * kFpStaging);
+    FpTail &tail = *(FpTail *)(smem + kFpStages * (kFpStage + kFpScales) + 2 * kFpStaging);
     volatile uint32_t &s_fail = tail.fail;
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
     const uint32_t ring = sm32(smem), staging = ring + kFpStages * kFpStage, scales = staging + 2 * kFpStaging;
@@ -347,8 +543,8 @@ __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __gri
                 if (s_fail) { ok = false; break; }
                 for (int kb = 0; kb < n_kb; ++kb) {
                     if (!__all_sync(0xFFFFFFFFu, gt_poll(empty0 + slot * 8u, par))) { ok = false; break; }
-                    const uint32_t with = (kb & 3) == 0 ? 1u : 0u, dst = ring + slot * kFpStage, sdst = scales + slot * kFsScaleBytes;
-                    const uint32_t bytes = 2u * (kFpStage + with * kFsScaleBytes), bar = lead_full0 + slot * 8u;
+                    const uint32_t with = (kb & 3) == 0 ? 1u : 0u, dst = ring + slot * kFpStage, sdst = scales + slot * kFpScales;
+                    const uint32_t bytes = 2u * (kFpStage + with * kFpScales), bar = lead_full0 + slot * 8u;
                     asm volatile("{\n .reg .pred e, l, s;\n elect.sync _|e, 0xFFFFFFFF;\n setp.eq.u32 l, %2, 0;\n and.pred l, l, e;\n setp.ne.b32 s, %3, 0;\n and.pred s, s, e;\n"
                                  " @l mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n"
                                  " @s cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%11], [%12, {%15, %13, %14}], [%4];\n"
@@ -377,7 +573,7 @@ __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __gri
             bool ok = true, full_now = false;
             for (int tile = t_first; tile < p.n_tiles && ok; tile += t_step) {
                 for (int kb = 0; kb < n_kb; ++kb) {
-                    const bool fresh = kF32 ? kb % kFpChunk == 0 : kb == 0;
+                    const bool fresh = kF32 ? kb % kFsChunk == 0 : kb == 0;
                     if (fresh) {
                         // the accumulator before this one has been read where they overlap, and the one before that altogether
                         if (unit > 0 && !gt_poll(sm32(&tail.acc_free), (unit - 1u) & 1u)) ok = false;
@@ -390,7 +586,7 @@ __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __gri
                     if (!full_now && !gt_poll_stage(full0 + slot * 8u, par)) { ok = false; break; }
                     const uint32_t with = (kb & 3) == 0 ? 1u : 0u;
                     if (with) set = (set + 1u) & (kFsSets - 1u);
-                    const uint32_t a16 = (ring + slot * kFpStage) >> 4, s16 = (scales + slot * kFsScaleBytes) >> 4;
+                    const uint32_t a16 = (ring + slot * kFpStage) >> 4, s16 = (scales + slot * kFpScales) >> 4;
                     const uint64_t da = kGtDesc | (uint64_t)(a16 & 0x3FFFu), db = kGtDesc | (uint64_t)((a16 + 1024u) & 0x3FFFu);
                     const uint64_t ds = kFsScaleDesc | (uint64_t)(s16 & 0x3FFFu);
                     const uint32_t fa = tmem + 448u + set * 16u, fb = fa + 8u, id = (uint32_t)kb & 3u, idesc = p.idesc | (id << 4) | (id << 29);
@@ -415,7 +611,7 @@ __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __gri
                                    "h"((unsigned short)3), "r"(full0 + (wrap ? 0u : slot + 1u) * 8u), "r"(wrap ? par ^ 1u : par) : "memory");
                     full_now = next != 0u;
                     if (wrap) { slot = 0; par ^= 1u; } else ++slot;
-                    if (kb + 1 == n_kb || (kF32 && (kb + 1) % kFpChunk == 0)) {
+                    if (kb + 1 == n_kb || (kF32 && (kb + 1) % kFsChunk == 0)) {
                         gt_commit_elected<true>(sm32(&tail.acc_full[unit & 1u]));
                         ++unit;
                     }
@@ -435,7 +631,7 @@ __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __gri
         const bool issuer = q == 0 && lane == 0;
         const float *bias_of = from_here(p.bias);
         const uint8_t *gamma = from_here(p.gamma);
-        const int chunks = kF32 ? (n_kb + kFpChunk - 1) / kFpChunk : 1;
+        const int chunks = kF32 ? (n_kb + kFsChunk - 1) / kFsChunk : 1;
         uint32_t unit = 0;
         bool ok = true;
         auto hand_back = [&]() {
@@ -552,6 +748,17 @@ bsp_status fs_map(CUtensorMap *map, const bsp_f8 &m, int box_rows)
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? BSP_OK : BSP_ERR_CUDA;
 }
 
+// Y as bytes in rows of `row` bytes, in boxes of 128 bytes x 128 rows.
+bsp_status fs_y_map(CUtensorMap *map, void *Y, int64_t rows, int64_t row)
+{
+    GtEncodeFn enc = gt_encode();
+    if (!enc) return BSP_ERR_CUDA;
+    const cuuint64_t gdim[2] = {(cuuint64_t)row, (cuuint64_t)rows}, gstr[1] = {(cuuint64_t)row};
+    const cuuint32_t box[2] = {128u, 128u}, estr[2] = {1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, Y, gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+               CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? BSP_OK : BSP_ERR_CUDA;
+}
+
 // Scales as a tensor of words: 128 words an atom, `atoms` atoms per 128 rows.
 bsp_status fp_scale_map(CUtensorMap *map, const bsp_f8 &m, int box_blocks)
 {
@@ -583,14 +790,137 @@ bsp_status launch_pairs(const bsp_f8 &x, const bsp_f8 &w, const float *bias, con
     if (rc == BSP_OK) rc = fs_map(&p.tmb, w, 128);
     if (rc == BSP_OK) rc = fp_scale_map(&p.tsa, x, 1);
     if (rc == BSP_OK) rc = fp_scale_map(&p.tsb, w, 2);
+    if (rc == BSP_OK) rc = fs_y_map(&p.tmy, Y, p.M, (int64_t)p.N * ey);
     if (rc != BSP_OK) return rc;
-    const cuuint64_t gdim[2] = {(cuuint64_t)p.N * ey, (cuuint64_t)p.M}, gstr[1] = {(cuuint64_t)p.N * ey};
-    const cuuint32_t box[2] = {128u, 128u}, estr[2] = {1, 1};
-    if (gt_encode()(&p.tmy, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, Y, gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                    CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-        return BSP_ERR_CUDA;
     const int pairs = p.n_tiles < sms / 2 ? p.n_tiles : sms / 2;
     BSP_CUDA_OK(launch_after_clusters(ey == 4 ? gemm_f8_pair_kernel<true> : gemm_f8_pair_kernel<false>, dim3((unsigned)(2 * pairs)), dim3(kFpThreads), kFpSmem, st, 2, 1, p));
+    return BSP_OK;
+}
+
+}  // namespace
+
+namespace {
+
+// What a device has room for: SMs, and clusters of 1, 2, 4 and 8 CTAs of the tile kernel at a time.
+struct FsDevice { int sms, clusters[4]; };
+bsp_status fs_device(FsDevice &d)
+{
+    static std::atomic<int> state[kGtMaxDevices];          // 0 unknown, 1 being written, 2 known
+    static FsDevice known[kGtMaxDevices];
+    int dev = 0;
+    BSP_CUDA_OK(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= kGtMaxDevices) return BSP_ERR_CUDA;
+    if (state[dev].load(std::memory_order_acquire) == 2) {
+        d = known[dev];
+        return BSP_OK;
+    }
+    d = {};
+    BSP_CUDA_OK(cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev));
+    void (*const tiles[3])(const FsParams) = {gemm_f8_tile_kernel<void>, gemm_f8_tile_kernel<float>, gemm_f8_tile_kernel<__nv_bfloat16>};
+    for (auto k : tiles) BSP_CUDA_OK(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kFsSmem));
+    BSP_CUDA_OK(cudaFuncSetAttribute(gemm_f8_pair_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFpSmem));
+    BSP_CUDA_OK(cudaFuncSetAttribute(gemm_f8_pair_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFpSmem));
+    for (int i = 0; i < 4; ++i) {
+        cudaLaunchAttribute at = {};
+        at.id = cudaLaunchAttributeClusterDimension;
+        at.val.clusterDim.x = 1u << i; at.val.clusterDim.y = at.val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(1024); cfg.blockDim = dim3(kFsThreads); cfg.dynamicSmemBytes = kFsSmem; cfg.attrs = &at; cfg.numAttrs = 1;
+        BSP_CUDA_OK(cudaOccupancyMaxActiveClusters(&d.clusters[i], gemm_f8_tile_kernel<void>, &cfg));
+    }
+    if (d.sms < 1 || d.clusters[0] < 1) return BSP_ERR_CUDA;
+    int none = 0;
+    if (state[dev].compare_exchange_strong(none, 1)) {
+        known[dev] = d;
+        state[dev].store(2, std::memory_order_release);
+    }
+    return BSP_OK;
+}
+
+// What FsParams and a choice of kernel follow from: x [M][K] times w [N][K], or, where `X` is given, its rows instead of x's.
+struct FsJob {
+    const bsp_f8 *x, *w;
+    const void *X;
+    bsp_dtype xtype;
+    int64_t P, ldx;
+    const float *bias;
+    const bsp_wdesc *wd;
+    const uint8_t *gamma;
+    void *Y;
+    bsp_dtype ytype;
+    void *ws;
+};
+
+// Columns of a tile and CTAs that share the summed axis: the pair with the lowest estimate in cycles.  A block of 128 entries costs its MMAs or
+// its loads, at about 50 bytes a clock and SM; a cluster its meeting.  (ring_bn: bytes of B in a stage, 0 where X is quantised in place.)
+struct FsChoice { int BN, split; double cycles; };
+constexpr int kFsPlaceRows = 768;                   // rows of 128 bytes of X that a CTA may hold where it quantises X itself
+FsChoice fs_choose(const FsDevice &d, int64_t M, int64_t N, int n_kb, bool transposed, bool in_place)
+{
+    FsChoice best = {0, 0, -1.0};
+    const int widths[4] = {16, 32, 64, 128};
+    for (int i = 0; i < 4; ++i) {
+        const int bn = widths[i];
+        if (transposed ? (bn < N || (i > 0 && widths[i - 1] >= N)) : (bn > 32 && widths[i - 1] >= N) || bn < 32) continue;
+        for (int j = 0; j < 4; ++j) {
+            const int split = 1 << j;
+            if (d.clusters[j] < 1 || (split > 1 && n_kb < 2 * split)) continue;
+            const double tiles = (double)f8_blocks(M) * (double)((N + bn - 1) / bn);
+            const double waves = tiles <= d.clusters[j] ? 1.0 : (double)(int64_t)((tiles + d.clusters[j] - 1) / d.clusters[j]);
+            const double mma = 4.0 * (32 + bn / 4 > bn / 2 ? 32 + bn / 4 : bn / 2), feed = 128.0 * (128 + (in_place ? 0 : bn)) / 50.0;
+            const int kb = (n_kb + split - 1) / split;
+            if (in_place && kb * bn > kFsPlaceRows) continue;
+            const double cycles = waves * (kb * (mma > feed ? mma : feed) + 2500.0 + 10.0 * bn + (split > 1 ? 1800.0 : 0.0));
+            if (best.cycles < 0 || cycles < best.cycles) best = {bn, split, cycles};
+        }
+    }
+    return best;
+}
+
+bsp_status launch_tiles(const FsDevice &d, const FsJob &j, const FsChoice &c, bool transposed, cudaStream_t st)
+{
+    FsParams p = {};
+    const int64_t K = j.w->cols, P = j.X ? j.P : j.x->rows;
+    p.transposed = transposed;
+    const bsp_f8 *a = transposed ? j.w : j.x, *b = transposed ? j.x : j.w;       // (b is NULL where X is quantised in place)
+    p.M = (int)(transposed ? j.w->rows : P); p.N = (int)(transposed ? P : j.w->rows);
+    p.BN = c.BN; p.split = c.split;
+    p.n_kb = (int)f8_blocks(K);
+    p.atoms = f8_atoms(K);
+    p.sa = (const uint8_t *)a->scale; p.sb = b ? (const uint8_t *)b->scale : nullptr;
+    const int64_t tiles_m = f8_blocks(p.M);
+    p.tiles_n = (p.N + p.BN - 1) / p.BN;
+    if (tiles_m * p.tiles_n * p.split > 0x7FFFFFFF) return BSP_ERR_SHAPE;
+    const int ey = j.ytype == BSP_BF16 ? 2 : 4, kb = (p.n_kb + p.split - 1) / p.split;
+    p.staged = !transposed && p.split == 1 && p.BN >= 64 && (int64_t)p.N * ey % 16 == 0;
+    // ring | X in 8 bits and its scales | shares of the cluster's CTAs | scales of the stages | barriers
+    p.stage_bytes = 16384 + (j.X ? 0 : p.BN * 128);
+    const int x_bytes = j.X ? kb * p.BN * 128 + (kb / 4 + 2) * kF8Atom : 0, recv = p.split > 1 ? p.BN * 512 : 0;
+    const int tail = (int)sizeof(FsTail);
+    p.stages = (kFsSmem - tail - x_bytes - recv) / (p.stage_bytes + kFsScales);
+    if (p.stages > kFsMaxStages) p.stages = kFsMaxStages;
+    if (p.stages > kb) p.stages = kb;
+    int ring = p.stages * p.stage_bytes;
+    if (p.staged && ring < p.BN * ey * 128) ring = p.BN * ey * 128;
+    p.off_x = ring; p.off_recv = ring + (x_bytes + 1023) / 1024 * 1024; p.off_scales = p.off_recv + recv; p.off_tail = p.off_scales + p.stages * kFsScales;
+    const int smem = p.off_tail + tail;
+    if (p.stages < 1 || smem > kFsSmem) return BSP_ERR_SHAPE;
+    // formats of A and B, N / 8, scales of 8 exponent bits, M / 128; both operands K-major
+    const uint32_t fa = a->type == BSP_E5M2 ? 1u : 0u, fb = b && b->type == BSP_E5M2 ? 1u : 0u;
+    p.idesc = (fa << 7) | (fb << 10) | ((uint32_t)(p.BN >> 3) << 17) | (1u << 23) | (1u << 27);
+    p.Y = (uint8_t *)j.Y; p.bf16 = j.ytype == BSP_BF16;
+    p.vec = p.N % 4 == 0;
+    p.bias = j.bias;
+    if (j.wd) { p.gamma = j.gamma; p.bo = f8_log2(j.wd->bo); p.bi = f8_log2(j.wd->bi); p.NBi = j.wd->I / j.wd->bi; }
+    p.X = j.X; p.ldx = j.ldx; p.K = K;
+    if (j.X) p.xvec = (uintptr_t)j.X % (4 * elem_bytes(j.xtype)) == 0 && j.ldx % 4 == 0;
+    p.status = (int *)j.ws;
+    bsp_status rc = fs_map(&p.tma, *a, 128);
+    if (rc == BSP_OK && b) rc = fs_map(&p.tmb, *b, p.BN);
+    if (rc == BSP_OK && p.staged) rc = fs_y_map(&p.tmy, j.Y, p.M, (int64_t)p.N * ey);
+    if (rc != BSP_OK) return rc;
+    const auto kernel = !j.X ? gemm_f8_tile_kernel<void> : j.xtype == BSP_F32 ? gemm_f8_tile_kernel<float> : gemm_f8_tile_kernel<__nv_bfloat16>;
+    BSP_CUDA_OK(launch_after_clusters(kernel, dim3((unsigned)(tiles_m * p.tiles_n * p.split)), dim3(kFsThreads), (size_t)smem, st, p.split, 1, p));
     return BSP_OK;
 }
 
@@ -599,61 +929,36 @@ bsp_status launch_pairs(const bsp_f8 &x, const bsp_f8 &w, const float *bias, con
 bsp_status launch_gemm_f8(const bsp_f8 &x, const bsp_f8 &w, const float *bias, const bsp_wdesc *wd, const uint8_t *gamma, void *Y, bsp_dtype ytype,
                           void *ws, cudaStream_t st)
 {
-    static int n_sm[kGtMaxDevices] = {};
-    static bool opted[kGtMaxDevices] = {};
-    int dev = 0;
-    BSP_CUDA_OK(cudaGetDevice(&dev));
-    if (dev < 0 || dev >= kGtMaxDevices) return BSP_ERR_CUDA;
-    if (!opted[dev]) {
-        BSP_CUDA_OK(cudaFuncSetAttribute(gemm_f8_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFsSmem));
-        BSP_CUDA_OK(cudaFuncSetAttribute(gemm_f8_pair_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFpSmem));
-        BSP_CUDA_OK(cudaFuncSetAttribute(gemm_f8_pair_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFpSmem));
-        opted[dev] = true;
-    }
-    if (n_sm[dev] == 0) BSP_CUDA_OK(cudaDeviceGetAttribute(&n_sm[dev], cudaDevAttrMultiProcessorCount, dev));
-    // large products, whose rows of Y a tensor map can describe
-    const long long pair_tiles = ((x.rows + 255) / 256) * ((w.rows + 255) / 256);
-    if (pair_tiles * 2 >= n_sm[dev] && w.rows * (ytype == BSP_BF16 ? 2 : 4) % 16 == 0 && n_sm[dev] >= 2)
-        return launch_pairs(x, w, bias, wd, gamma, Y, ytype, ws, n_sm[dev], st);
-    FsParams p = {};
-    // few rows of x become the columns of the MMA, whose rows are then the channels
-    p.transposed = wd == nullptr && x.rows <= 64;
-    const bsp_f8 &a = p.transposed ? w : x, &b = p.transposed ? x : w;
-    p.M = (int)a.rows; p.N = (int)b.rows;
-    p.n_kb = (int)f8_blocks(x.cols);
-    p.atoms = f8_atoms(x.cols);
-    p.sa = (const uint8_t *)a.scale; p.sb = (const uint8_t *)b.scale;
-    const long long tiles_m = f8_blocks(p.M);
-    p.BN = p.N <= 16 ? 16 : p.N <= 32 ? 32 : p.N <= 64 ? 64 : 128;
-    if (tiles_m * ((p.N + 255) / 256) >= n_sm[dev]) p.BN = 256;
-    p.tiles_n = (p.N + p.BN - 1) / p.BN;
-    const long long tiles = tiles_m * p.tiles_n;
-    p.split = 1;
-    while (p.split < 8 && tiles * p.split * 2 <= n_sm[dev] && p.n_kb >= p.split * 2 * 2) p.split *= 2;
-    if (tiles * p.split > 0x7FFFFFFF) return BSP_ERR_SHAPE;
-    p.stage_bytes = 16384 + p.BN * 128;
-    // the ring; the accumulators of a tile lie in it afterwards
-    const int tail = (int)sizeof(FsTail), per_stage = p.stage_bytes + kFsScaleBytes;
-    p.stages = (kFsSmem - tail) / per_stage;
-    if (p.stages > kFsMaxStages) p.stages = kFsMaxStages;
-    const int part = p.transposed ? p.BN * 512 : 128 * (p.BN + 4) * 4;
-    const int want = (p.n_kb + p.split - 1) / p.split;
-    if (p.stages > want) p.stages = want;
-    while (p.stages * p.stage_bytes < part) ++p.stages;
-    const size_t smem = (size_t)p.stages * per_stage + tail;
-    const uint32_t fa = a.type == BSP_E5M2 ? 1u : 0u, fb = b.type == BSP_E5M2 ? 1u : 0u;
-    // formats of A and B, N / 8, scales of 8 exponent bits, M / 128; both operands K-major
-    p.idesc = (fa << 7) | (fb << 10) | ((uint32_t)(p.BN >> 3) << 17) | (1u << 23) | (1u << 27);
-    p.Y = (uint8_t *)Y; p.bf16 = ytype == BSP_BF16;
-    p.vec = (p.transposed ? p.M : p.N) % 4 == 0;
-    p.bias = bias;
-    if (wd) { p.gamma = gamma; p.bo = wd->bo; p.bi = wd->bi; p.NBi = wd->I / wd->bi; }
-    p.status = (int *)ws;
-    bsp_status rc = fs_map(&p.tma, a, 128);
-    if (rc == BSP_OK) rc = fs_map(&p.tmb, b, p.BN);
+    FsDevice d;
+    const bsp_status rc = fs_device(d);
     if (rc != BSP_OK) return rc;
-    BSP_CUDA_OK(launch_after_clusters(gemm_f8_kernel, dim3((unsigned)(tiles * p.split)), dim3(kFsThreads), smem, st, p.split, 1, p));
-    return BSP_OK;
+    // few rows of x become the columns of the MMA, whose rows are then the channels
+    const bool transposed = wd == nullptr && x.rows <= 64;
+    const int n_kb = (int)f8_blocks(x.cols);
+    const FsChoice c = fs_choose(d, transposed ? w.rows : x.rows, transposed ? x.rows : w.rows, n_kb, transposed, false);
+    // pairs of CTAs, where a tensor map can describe the rows of Y
+    const double tiles = (double)((x.rows + 255) / 256) * (double)((w.rows + 255) / 256), pairs = d.sms / 2;
+    if (!transposed && d.sms >= 2 && w.rows * (ytype == BSP_BF16 ? 2 : 4) % 16 == 0) {
+        const double cycles = (double)(int64_t)((tiles + pairs - 1) / pairs) * (n_kb * 690.0 + 1500.0) + 4500.0;
+        if (cycles < c.cycles) return launch_pairs(x, w, bias, wd, gamma, Y, ytype, ws, d.sms, st);
+    }
+    return launch_tiles(d, FsJob{&x, &w, nullptr, BSP_F32, 0, 0, bias, wd, gamma, Y, ytype, ws}, c, transposed, st);
+}
+
+// Few rows of X are quantised by the CTAs that multiply them (each its share of the channels, again for every 128 channels of the output),
+// others go through `x`, which lies in the workspace.
+bsp_status launch_linear_f8(const bsp_f8 &w, const void *X, bsp_dtype xtype, int64_t P, int64_t ldx, const bsp_f8 &x, const float *bias, void *Y,
+                            bsp_dtype ytype, void *ws, cudaStream_t st)
+{
+    FsDevice d;
+    bsp_status rc = fs_device(d);
+    if (rc != BSP_OK) return rc;
+    if (P <= 64) {
+        const FsChoice c = fs_choose(d, w.rows, P, (int)f8_blocks(w.cols), true, true);
+        if (c.cycles >= 0) return launch_tiles(d, FsJob{nullptr, &w, X, xtype, P, ldx, bias, nullptr, nullptr, Y, ytype, ws}, c, true, st);
+    }
+    rc = launch_quantize_f8(X, xtype, P, w.cols, ldx, nullptr, nullptr, &x, nullptr, nullptr, ws, st);
+    return rc != BSP_OK ? rc : launch_gemm_f8(x, w, bias, nullptr, nullptr, Y, ytype, ws, st);
 }
 
 }  // namespace bsp

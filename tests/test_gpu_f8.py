@@ -209,6 +209,17 @@ def test_gemm_scales_across_their_range():
     assert (np.abs(got - want) <= product_bound(a, b, want, "f32")).all()
 
 
+@pytest.mark.parametrize("M,N,K,out", [(40, 200, 20000, "f32"), (100, 32, 9000, "f32"), (128, 64, 3000, "bf16"), (70, 61, 5000, "f32"), (500, 66, 300, "bf16"), (700, 1026, 128, "f32"),
+                                       (5000, 136, 2304, "f32"), (300, 7, 2000, "bf16")])
+def test_gemm_shared_sums_and_narrow_tiles(M, N, K, out):
+    """Long sums over clusters and in several chunks, tiles of every width, outputs whose rows are not 16-byte multiples."""
+    A, a = random_held(3060 + M, M, K, "e4m3")
+    B, b = random_held(3160 + N, N, K, "e5m2", 0.05)
+    bias = synth.normal(3260, (N,), 1.0).astype(np.float32)
+    got, want = gemm(A, a, B, b, bias, out)
+    assert (np.abs(got - want) <= product_bound(a, b, want, out)).all()
+
+
 def test_gemm_nan_stays_in_its_row_and_column():
     M, N, K = 150, 140, 260
     codes, s = f8.quantize(values(3400, M, K, "f32"), "e4m3")
@@ -272,6 +283,42 @@ def test_linear(P, I, O, dtype, out):
     bsp.bsp_check(ws)
     want = a @ b.T + bias.astype(np.float64)
     assert (np.abs(Y.float().cpu().numpy() - want) <= product_bound(a, b, want, out)).all()
+
+
+@pytest.mark.parametrize("P,I,O", [(64, 40000, 136), (2, 70000, 24), (64, 8192, 4100), (40, 129, 128)])
+def test_linear_long_rows(P, I, O):
+    """Rows that a CTA cannot hold in 8 bits, and ones that it can."""
+    x = values(3950 + P, P, I, "bf16")
+    B, b = random_held(3951 + O, O, I, "e4m3", 0.05)
+    a = f8.dequantize(*f8.quantize(x, "e4m3"), "e4m3")
+    Y = torch.full((P, O), -7.0, device="cuda")
+    ws = bsp.new_workspace(bsp.bsp_linear_f8_workspace_bytes(B.m, P))
+    bsp.bsp_linear_f8(B.m, device(x, "bf16"), bsp.BF16, P, I, None, Y, bsp.F32, ws)
+    bsp.bsp_check(ws)
+    want = a @ b.T
+    assert (np.abs(Y.cpu().numpy() - want) <= product_bound(a, b, want, "f32")).all()
+
+
+def test_linear_extremes():
+    """NaN, infinities, zeros and subnormals in the rows that a server hands over come out as from the quantiser and the product."""
+    P, I, O = 9, 1000, 200
+    x = values(3960, P, I, "f32")
+    x[1] = 0.0
+    x[2, 5], x[3, 700], x[4, 130] = np.nan, np.inf, -np.inf
+    x[5] = 2.0 ** -140
+    x[6] = np.inf
+    B, b = random_held(3961, O, I, "e4m3", 0.05)
+    lay = bsp.F8Layer(O, I, 8, 8, torch.float32)
+    lay.w.data.copy_(B.data); lay.w.scale.copy_(B.scale)
+    Y, act, Z = torch.empty((P, O), device="cuda"), bsp.F8Activations(P, I), torch.empty((P, O), device="cuda")
+    lay.linear(device(x, "f32"), None, Y)
+    lay.forward(device(x, "f32"), act, None, Z)
+    a = f8.dequantize(*f8.quantize(x, "e4m3"), "e4m3")
+    bad = np.isnan(a).any(1)
+    for got in (Y.cpu().numpy(), Z.cpu().numpy()):
+        assert np.isnan(got[bad]).all() and np.isfinite(got[~bad]).all()
+        want = a[~bad] @ b.T
+        assert (np.abs(got[~bad] - want) <= product_bound(a[~bad], b, want, "f32")).all()
 
 
 def step_tensors(P, O, I):

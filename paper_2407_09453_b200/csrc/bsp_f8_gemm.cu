@@ -37,21 +37,21 @@ struct FsParams {
     int off_x, off_recv, off_scales, off_tail;      // offsets in shared memory
     uint32_t idesc;
     uint8_t *Y;
-    int bf16, transposed, vec;    // element (m, n) at Y[m N + n], or at Y[n M + m]; rows that can be written 16 bytes at a time
+    int bf16, transposed, vec;    // element (m, n) at Y[m N + n], or at Y[n M + m]; rows that can be written four entries at a time
     int staged;                   // the output leaves by TMA stores
     const float *bias;
     const uint8_t *gamma;
     int bo, bi, NBi;              // Gamma's blocks: logarithms of their sizes, blocks in a row
     const void *X;                // kX: the rows of B before they are quantised, ldx entries apart
     int64_t ldx, K;
-    int xvec;                     // rows of X can be read four entries at a time
+    int xvec;                     // rows of X can be read 16 bytes at a time
     int *status;
 };
 
 struct FsTail {
-    uint64_t full[kFsMaxStages], empty[kFsMaxStages], acc_full[2], acc_free[2], x_ready;
+    uint64_t full[kFsMaxStages], empty[kFsMaxStages], acc_full[2], acc_free[2], x_ready, shares;
     uint32_t tmem, fail;
-    float bias[128];
+    __align__(16) float bias[128];
 };
 
 // 16 consecutive accumulator columns of this thread's tensor-memory lane.
@@ -66,25 +66,26 @@ __device__ __forceinline__ void fs_load16(uint32_t taddr, uint32_t (&v)[16])
                    "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]) :: "memory");
 }
 
-// Four entries of a row of X, `n` of which exist.
-__device__ __forceinline__ void fs_load_x(const float *x, int64_t n, int vec, float (&v)[4])
+// Eight entries of a row of X, `n` of which exist.
+__device__ __forceinline__ void fs_load_x(const float *x, int64_t n, int vec, float (&v)[8])
 {
-    if (vec && n >= 4) {
-        const float4 a = load_free((const float4 *)x);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    if (vec && n >= 8) {
+        const float4 a = load_free((const float4 *)x), b = load_free<16>((const float4 *)x);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
     } else
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = i < n ? __uint_as_float(load_free((const uint32_t *)x + i)) : 0.f;
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? __uint_as_float(load_free((const uint32_t *)x + i)) : 0.f;
 }
-__device__ __forceinline__ void fs_load_x(const __nv_bfloat16 *x, int64_t n, int vec, float (&v)[4])
+__device__ __forceinline__ void fs_load_x(const __nv_bfloat16 *x, int64_t n, int vec, float (&v)[8])
 {
-    if (vec && n >= 4) {
-        const uint2 a = load_free((const uint2 *)x);
-        v[0] = __uint_as_float(a.x << 16); v[1] = __uint_as_float(a.x & 0xFFFF0000u);
-        v[2] = __uint_as_float(a.y << 16); v[3] = __uint_as_float(a.y & 0xFFFF0000u);
+    if (vec && n >= 8) {
+        const uint4 a = load_free((const uint4 *)x);
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
     } else
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = i < n ? __bfloat162float(x[i]) : 0.f;
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? __bfloat162float(x[i]) : 0.f;
 }
 
 // What an element becomes, two neighbours of a row at a time.
@@ -94,8 +95,8 @@ __device__ __forceinline__ uint32_t fs_pack(float lo, float hi)
     return *(const uint32_t *)&h;
 }
 
-// One tile of 128 x BN per cluster.  CTA r of the cluster sums its share of the blocks, sends the columns that CTA s stores to s through
-// distributed shared memory, and s adds the shares up in the order of the ranks: every CTA stores BN / split columns of the tile.
+// One tile of 128 x BN per cluster.  CTA r of the cluster sums its share of the blocks and sends the rows of the output that CTA s stores to s
+// (one bulk copy between their shared memories); s adds the shares up in the order of the ranks.
 // (A cluster of eight finds room for 15 of its kind on the 148 SMs, of four for 33, of two for 74.)
 // Chunks of kFsChunk blocks go to two accumulators in turn and are added up in registers (256 instructions in a row into one
 // accumulator, 8192 entries, were off by 1.9e-6 of the result, chunks by 5.5e-7; plain float32 sums by 4.2e-7).
@@ -125,6 +126,7 @@ __global__ void __launch_bounds__(kFsThreads, 1) gemm_f8_tile_kernel(const __gri
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(sm32(&tail.acc_free[b])), "r"(8) : "memory");
         }
         asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(sm32(&tail.x_ready)), "r"(8) : "memory");
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(sm32(&tail.shares)), "r"(1) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         s_fail = (ring & 1023u) == 0u ? 0u : 2u;
         asm volatile("prefetch.tensormap [%0];\n" ::"l"(&p.tma) : "memory");
@@ -140,8 +142,17 @@ __global__ void __launch_bounds__(kFsThreads, 1) gemm_f8_tile_kernel(const __gri
     asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+    // the bytes that the other CTAs of the cluster will send
+    // (lines: rows of the output in this tile; `per` of them to a CTA)
+    const int valid_n = p.N - n0 < BN ? p.N - n0 : BN, valid_m = p.M - m0 < 128 ? p.M - m0 : 128;
+    const int lines = p.transposed ? valid_n : valid_m, per = (p.transposed ? BN : 128) / split, line_bytes = p.transposed ? 512 : BN * 4;
+    if (split > 1 && tid == 0) {
+        const int n = lines - rank * per < per ? lines - rank * per : per;
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(sm32(&tail.shares)), "r"(n > 0 ? (uint32_t)((split - 1) * n * line_bytes) : 0u) : "memory");
+    }
+    __syncwarp();
     // (the CTAs of a cluster run once this barrier is complete: what they send each other waits for it)
-    if (split > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;\n" ::: "memory");
+    if (split > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
     const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, tail.tmem, 0), sf = tmem + cols - 64u;
     const bool run = __shfl_sync(0xFFFFFFFFu, s_fail, 0) == 0u;
     const uint32_t full0 = sm32(&tail.full[0]), empty0 = sm32(&tail.empty[0]);
@@ -238,49 +249,59 @@ __global__ void __launch_bounds__(kFsThreads, 1) gemm_f8_tile_kernel(const __gri
     } else if (run) {
         const int w = warp - 2, q = warp & 3, grp = w >> 2;
         if constexpr (kX) {
-            // ================= rows of X to 8 bits: a warp takes 128 entries of a row, four to a lane =================
+            // ================= rows of X to 8 bits: half a warp takes 128 entries of a row, eight to a lane =================
             const T *X = from_here((const T *)p.X);
-            const int rows = p.N < BN ? p.N : BN, items = (kb1 - kb0) * rows;
-            constexpr int kBatch = 4;
-            for (int i0 = w; i0 < items; i0 += 8 * kBatch) {
-                float v[kBatch][4], m[kBatch];
+            const int rows = p.N < BN ? p.N : BN, items = (kb1 - kb0) * rows, l = lane & 15;
+            const uint32_t recip = 65536u / (uint32_t)rows + 1u;          // (items are at most 768: the quotient is exact)
+            auto pass = [&](auto batch_c) {
+            constexpr int kBatch = decltype(batch_c)::value;            // (items in flight; what lies past the last is worked on too)
+            for (int i0 = w * 2 + (lane >> 4); i0 - (lane >> 4) < items; i0 += 16 * kBatch) {
+                float v[kBatch][8], m[kBatch];
 #pragma unroll
                 for (int u = 0; u < kBatch; ++u) {
-                    const int i = i0 + 8 * u, b = i / rows, r = i - b * rows;
-                    const int64_t c = (int64_t)(kb0 + b) * kF8Block + lane * 4;
+                    const int i = i0 + 16 * u, b = (int)((uint32_t)i * recip >> 16), r = i - b * rows;
+                    const int64_t c = (int64_t)(kb0 + b) * kF8Block + l * 8;
                     fs_load_x(X + r * p.ldx + c, i < items ? p.K - c : 0, p.xvec, v[u]);
                 }
 #pragma unroll
-                for (int u = 0; u < kBatch; ++u) m[u] = fmaxf(fmaxf(fabsf(v[u][0]), fabsf(v[u][1])), fmaxf(fabsf(v[u][2]), fabsf(v[u][3])));
+                for (int u = 0; u < kBatch; ++u) {
+                    m[u] = fabsf(v[u][0]);
 #pragma unroll
-                for (int d = 16; d > 0; d >>= 1)
+                    for (int e = 1; e < 8; ++e) m[u] = fmaxf(m[u], fabsf(v[u][e]));
+                    m[u] = fmaxf(m[u], 0.f);
+                }
+#pragma unroll
+                for (int d = 8; d > 0; d >>= 1)
 #pragma unroll
                     for (int u = 0; u < kBatch; ++u) m[u] = fmaxf(m[u], __shfl_xor_sync(0xFFFFFFFFu, m[u], d));
 #pragma unroll
                 for (int u = 0; u < kBatch; ++u) {
-                    const int i = i0 + 8 * u, b = i / rows, r = i - b * rows;
-                    if (m[u] == __uint_as_float(0x7F800000u)) {        // (infinities become NaN and enter no scale)
+                    const int i = i0 + 16 * u, b = (int)((uint32_t)i * recip >> 16), r = i - b * rows;
+                    if (__any_sync(0xFFFFFFFFu, m[u] == __uint_as_float(0x7F800000u))) {        // (infinities become NaN and enter no scale)
                         m[u] = 0.f;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
+                        for (int e = 0; e < 8; ++e) {
                             if (fabsf(v[u][e]) == __uint_as_float(0x7F800000u)) v[u][e] = __uint_as_float(0x7FFFFFFFu);
                             m[u] = fmaxf(m[u], fabsf(v[u][e]));
                         }
 #pragma unroll
-                        for (int d = 16; d > 0; d >>= 1) m[u] = fmaxf(m[u], __shfl_xor_sync(0xFFFFFFFFu, m[u], d));
+                        for (int d = 8; d > 0; d >>= 1) m[u] = fmaxf(m[u], __shfl_xor_sync(0xFFFFFFFFu, m[u], d));
                     }
                     const uint32_t byte = f8_scale_byte<false>(__float_as_uint(m[u]));
                     const float f = f8_inverse(byte);
                     if (i < items) {
-                        const uint32_t word = f8_pack<false>(v[u][0] * f, v[u][1] * f) | f8_pack<false>(v[u][2] * f, v[u][3] * f) << 16;
+                        const uint32_t lo = f8_pack<false>(v[u][0] * f, v[u][1] * f) | f8_pack<false>(v[u][2] * f, v[u][3] * f) << 16;
+                        const uint32_t hi = f8_pack<false>(v[u][4] * f, v[u][5] * f) | f8_pack<false>(v[u][6] * f, v[u][7] * f) << 16;
                         const uint32_t row = xs + (uint32_t)(b * BN * 128 + r * 128);
-                        asm volatile("st.shared.b32 [%0], %1;\n" ::"r"(row + ((((uint32_t)lane >> 2) ^ ((uint32_t)r & 7u)) << 4) + ((uint32_t)lane & 3u) * 4u), "r"(word) : "memory");
-                        if (lane == 0)
+                        asm volatile("st.shared.v2.b32 [%0], {%1, %2};\n" ::"r"(row + ((((uint32_t)l >> 1) ^ ((uint32_t)r & 7u)) << 4) + ((uint32_t)l & 1u) * 8u), "r"(lo), "r"(hi) : "memory");
+                        if (l == 0)
                             asm volatile("st.shared.u8 [%0], %1;\n" ::"r"(xs_scales + (uint32_t)(((kb0 + b) >> 2) - (kb0 >> 2)) * kF8Atom +
                                                                          (uint32_t)((r & 31) * 16 + (r >> 5) * 4 + ((kb0 + b) & 3))), "r"(byte) : "memory");
                     }
                 }
             }
+            };
+            if (items <= 32) pass(std::integral_constant<int, 2>()); else pass(std::integral_constant<int, 8>());
             asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
             __syncwarp();
             if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(sm32(&tail.x_ready)) : "memory");
@@ -313,68 +334,79 @@ __global__ void __launch_bounds__(kFsThreads, 1) gemm_f8_tile_kernel(const __gri
     }
     // ================= the shares to the CTAs that store them =================
     __syncwarp();
-    const int valid_n = p.N - n0 < BN ? p.N - n0 : BN, per = BN / split, row = (warp & 3) * 32 + lane, grp = (warp - 2) >> 2;
+    const int row = (warp & 3) * 32 + lane, grp = (warp - 2) >> 2;
     const int first = grp * (BN / 2), pieces = BN >= 32 ? BN / 32 : 1 - grp;
     const bool epilogue = warp >= 2;
     if (split > 1) {
         asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
-        if (epilogue && run) {
-            // at the receiver: [rank of the sender][its column][128 rows]
-            const uint32_t mine = ring + (uint32_t)p.off_recv + (uint32_t)(rank * per * 128 + row) * 4u;
+        if (epilogue) {
+            // the tile by lines to the ring, which is free; the lines that another CTA stores go to it in one copy, to the place of this rank
+            // (lines of BN entries: 16-byte piece j of line r at place j ^ (r % 8), so that the lanes, a line each, meet different banks)
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (k < pieces)
+                if (k < pieces) {
+                    if (p.transposed) {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int c = first + k * 16 + e, to = c / per;
-                        if (c < valid_n)
-                            asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %0, %1;\n st.shared::cluster.f32 [a], %2;\n}\n"
-                                         ::"r"(mine + (uint32_t)(c - to * per) * 512u), "r"(to), "f"(acc[k][e]) : "memory");
+                        for (int e = 0; e < 16; ++e)
+                            asm volatile("st.shared.f32 [%0], %1;\n" ::"r"(ring + (uint32_t)((first + k * 16 + e) * 128 + row) * 4u), "f"(acc[k][e]) : "memory");
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};\n" ::"r"(ring + (uint32_t)(row * line_bytes) + ((((uint32_t)(first + k * 16) >> 2) + e) ^ ((uint32_t)row & 7u)) * 16u),
+                                         "f"(acc[k][4 * e]), "f"(acc[k][4 * e + 1]), "f"(acc[k][4 * e + 2]), "f"(acc[k][4 * e + 3]) : "memory");
                     }
+                }
+            asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+            asm volatile("bar.sync 1, 256;\n" ::: "memory");
+            const int to = tid - 64, n = lines - to * per < per ? lines - to * per : per;
+            if (run && to < split && to != rank && n > 0)
+                asm volatile("{\n .reg .b32 a, b;\n mapa.shared::cluster.u32 a, %0, %1;\n mapa.shared::cluster.u32 b, %2, %1;\n"
+                             " cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [a], [%3], %4, [b];\n}\n"
+                             ::"r"(ring + (uint32_t)p.off_recv + (uint32_t)(rank * per * line_bytes)), "r"(to), "r"(sm32(&tail.shares)), "r"(ring + (uint32_t)(to * per * line_bytes)),
+                               "r"((uint32_t)(n * line_bytes)) : "memory");
+            if (run && !gt_wait(sm32(&tail.shares), 0u)) atomicExch(&tail.fail, 1u);
+            __syncwarp();
         }
-        asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+        // (complete once all shares have arrived everywhere: no CTA leaves while its memory is still read)
+        asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
     } else __syncthreads();
-    // (whoever gave up did so before the barrier: all warps see the same)
+    // (without a cluster whoever gave up did so before the barrier, and all warps see the same; with one no barrier of the CTA alone follows)
     const bool fine = run && s_fail == 0u;
     const uint8_t *gamma = from_here(p.gamma);
     const int ey = p.bf16 ? 2 : 4;
     if (!epilogue || !fine) {
     } else if (split > 1) {
-        const int c0 = rank * per, n = valid_n - c0 < per ? valid_n - c0 : per;        // columns of this CTA's share
-        const float *recv = (const float *)(smem + p.off_recv);
-        const int m = (tid - 64) & 127, half = (tid - 64) >> 7;
-        auto sum = [&](int c) {
-            float v = recv[c * 128 + m];
-            for (int s = 1; s < split; ++s) v += recv[(s * per + c) * 128 + m];
-            return v;
-        };
-        if (m0 + m < p.M) {
-            if (p.transposed)
-                for (int c = half; c < n; c += 2) {
-                    const float v = sum(c) + tail.bias[m];
-                    const int64_t at = (int64_t)(n0 + c0 + c) * p.M + m0 + m;
-                    if (p.bf16) ((__nv_bfloat16 *)p.Y)[at] = __float2bfloat16_rn(v);
-                    else ((float *)p.Y)[at] = v;
-                }
-            else
-                for (int c = half * 4; c < n; c += 8) {
-                    float v[4];
+        // four entries of a line to a thread, the shares in the order of the ranks
+        const int l0 = rank * per, n = lines - l0 < per ? lines - l0 : per, shift = p.transposed ? 5 : 31 - __clz(BN >> 2);
+        const int in0 = p.transposed ? m0 : n0, in_end = p.transposed ? p.M : p.N, lead0 = p.transposed ? n0 : m0;
+        const uint32_t own = ring + (uint32_t)(l0 * line_bytes), recv = ring + (uint32_t)p.off_recv, share = (uint32_t)(per * line_bytes);
+        for (int u = tid - 64; u < n << shift; u += 256) {
+            const int l = u >> shift, j = u - (l << shift), in = in0 + j * 4;
+            if (in >= in_end) continue;
+            const uint32_t at = (uint32_t)(l * line_bytes) + (uint32_t)(p.transposed ? j : j ^ ((l0 + l) & 7)) * 16u;
+            float4 w[8];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = c + e < n ? sum(c + e) + tail.bias[c0 + c + e] : 0.f;
-                    const int col = n0 + c0 + c;
-                    if (gamma != nullptr && load_free(gamma + (int64_t)((m0 + m) >> p.bo) * p.NBi + (col >> p.bi)) == 0u) v[0] = v[1] = v[2] = v[3] = 0.f;
-                    const int64_t at = (int64_t)(m0 + m) * p.N + col;
-                    if (p.vec && c + 4 <= n) {
-                        if (p.bf16) *(uint2 *)((__nv_bfloat16 *)p.Y + at) = make_uint2(fs_pack(v[0], v[1]), fs_pack(v[2], v[3]));
-                        else *(float4 *)((float *)p.Y + at) = make_float4(v[0], v[1], v[2], v[3]);
-                    } else
+            for (int s = 0; s < 8; ++s)
+                if (s < split)
+                    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];\n" : "=f"(w[s].x), "=f"(w[s].y), "=f"(w[s].z), "=f"(w[s].w) : "r"((s == rank ? own : recv + (uint32_t)s * share) + at));
+            float v[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (c + e < n) {
-                                if (p.bf16) ((__nv_bfloat16 *)p.Y)[at + e] = __float2bfloat16_rn(v[e]);
-                                else ((float *)p.Y)[at + e] = v[e];
-                            }
-                }
+            for (int s = 1; s < 8; ++s)
+                if (s < split) { v[0] += w[s].x; v[1] += w[s].y; v[2] += w[s].z; v[3] += w[s].w; }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += tail.bias[j * 4 + e];
+            if (gamma != nullptr && load_free(gamma + (int64_t)((lead0 + l0 + l) >> p.bo) * p.NBi + (in >> p.bi)) == 0u) v[0] = v[1] = v[2] = v[3] = 0.f;
+            const int64_t out = (int64_t)(lead0 + l0 + l) * in_end + in;
+            if (p.vec) {
+                if (p.bf16) *(uint2 *)((__nv_bfloat16 *)p.Y + out) = make_uint2(fs_pack(v[0], v[1]), fs_pack(v[2], v[3]));
+                else *(float4 *)((float *)p.Y + out) = make_float4(v[0], v[1], v[2], v[3]);
+            } else
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (in + e < in_end) {
+                        if (p.bf16) ((__nv_bfloat16 *)p.Y)[out + e] = __float2bfloat16_rn(v[e]);
+                        else ((float *)p.Y)[out + e] = v[e];
+                    }
         }
     } else {
         const int m = m0 + row;
@@ -447,7 +479,8 @@ __global__ void __launch_bounds__(kFsThreads, 1) gemm_f8_tile_kernel(const __gri
     }
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
-    __syncthreads();
+    if (split > 1) asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+    else __syncthreads();
     if (s_fail == 1u && tid == 0) atomicMax(p.status, (int)BSP_ERR_TIMEOUT);
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(cols) : "memory");
 }
@@ -852,7 +885,8 @@ struct FsJob {
 };
 
 // Columns of a tile and CTAs that share the summed axis: the pair with the lowest estimate in cycles.  A block of 128 entries costs its MMAs or
-// its loads, at about 50 bytes a clock and SM; a cluster its meeting.  (ring_bn: bytes of B in a stage, 0 where X is quantised in place.)
+// its loads, at about 50 bytes a clock and SM; what comes before and after was measured by phases (1023 x 2048 x 1000 and 1024 x 12544 x 256: 4600
+// cycles for 64 columns without a cluster; 7100 for 64 over four CTAs and 10700 for 128 over two, whose shares take 0.6 cycles an entry).
 struct FsChoice { int BN, split; double cycles; };
 constexpr int kFsPlaceRows = 768;                   // rows of 128 bytes of X that a CTA may hold where it quantises X itself
 FsChoice fs_choose(const FsDevice &d, int64_t M, int64_t N, int n_kb, bool transposed, bool in_place)
@@ -870,7 +904,7 @@ FsChoice fs_choose(const FsDevice &d, int64_t M, int64_t N, int n_kb, bool trans
             const double mma = 4.0 * (32 + bn / 4 > bn / 2 ? 32 + bn / 4 : bn / 2), feed = 128.0 * (128 + (in_place ? 0 : bn)) / 50.0;
             const int kb = (n_kb + split - 1) / split;
             if (in_place && kb * bn > kFsPlaceRows) continue;
-            const double cycles = waves * (kb * (mma > feed ? mma : feed) + 2500.0 + 10.0 * bn + (split > 1 ? 1800.0 : 0.0));
+            const double cycles = waves * (kb * (mma > feed ? mma : feed) + (split > 1 ? 6000.0 + 73.0 * bn / split : 2600.0 + 16.0 * bn));
             if (best.cycles < 0 || cycles < best.cycles) best = {bn, split, cycles};
         }
     }
@@ -902,6 +936,7 @@ bsp_status launch_tiles(const FsDevice &d, const FsJob &j, const FsChoice &c, bo
     if (p.stages > kb) p.stages = kb;
     int ring = p.stages * p.stage_bytes;
     if (p.staged && ring < p.BN * ey * 128) ring = p.BN * ey * 128;
+    if (p.split > 1 && ring < p.BN * 512) ring = p.BN * 512;
     p.off_x = ring; p.off_recv = ring + (x_bytes + 1023) / 1024 * 1024; p.off_scales = p.off_recv + recv; p.off_tail = p.off_scales + p.stages * kFsScales;
     const int smem = p.off_tail + tail;
     if (p.stages < 1 || smem > kFsSmem) return BSP_ERR_SHAPE;
@@ -909,11 +944,11 @@ bsp_status launch_tiles(const FsDevice &d, const FsJob &j, const FsChoice &c, bo
     const uint32_t fa = a->type == BSP_E5M2 ? 1u : 0u, fb = b && b->type == BSP_E5M2 ? 1u : 0u;
     p.idesc = (fa << 7) | (fb << 10) | ((uint32_t)(p.BN >> 3) << 17) | (1u << 23) | (1u << 27);
     p.Y = (uint8_t *)j.Y; p.bf16 = j.ytype == BSP_BF16;
-    p.vec = p.N % 4 == 0;
+    p.vec = (transposed ? p.M : p.N) % 4 == 0;
     p.bias = j.bias;
     if (j.wd) { p.gamma = j.gamma; p.bo = f8_log2(j.wd->bo); p.bi = f8_log2(j.wd->bi); p.NBi = j.wd->I / j.wd->bi; }
     p.X = j.X; p.ldx = j.ldx; p.K = K;
-    if (j.X) p.xvec = (uintptr_t)j.X % (4 * elem_bytes(j.xtype)) == 0 && j.ldx % 4 == 0;
+    if (j.X) p.xvec = (uintptr_t)j.X % 16 == 0 && j.ldx * elem_bytes(j.xtype) % 16 == 0;
     p.status = (int *)j.ws;
     bsp_status rc = fs_map(&p.tma, *a, 128);
     if (rc == BSP_OK && b) rc = fs_map(&p.tmb, *b, p.BN);

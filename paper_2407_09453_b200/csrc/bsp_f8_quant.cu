@@ -309,83 +309,96 @@ struct DParams {
     int vec;
 };
 
-// Eight entries in a row of X; `n` of them exist.
-__device__ __forceinline__ void d_store8(__nv_bfloat16 *x, const float (&v)[8], int n, int vec)
+// 16 bytes of a row of X (eight bfloat16 entries, four float32); `n` entries exist.
+__device__ __forceinline__ void d_store(__nv_bfloat16 *x, const float (&v)[8], int n, int vec)
 {
     if (vec && n >= 8) {
-        uint4 w;
-        uint32_t *o = &w.x;
+        uint32_t o[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
             o[i] = *(const uint32_t *)&h;
         }
-        *(uint4 *)x = w;
+        *(uint4 *)x = make_uint4(o[0], o[1], o[2], o[3]);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (i < n) x[i] = __float2bfloat16_rn(v[i]);
     }
 }
-__device__ __forceinline__ void d_store8(float *x, const float (&v)[8], int n, int vec)
+__device__ __forceinline__ void d_store(float *x, const float (&v)[4], int n, int vec)
 {
-    if (vec && n >= 8) {
-        *(float4 *)x = make_float4(v[0], v[1], v[2], v[3]);
-        *(float4 *)(x + 4) = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
+    if (vec && n >= 4) *(float4 *)x = make_float4(v[0], v[1], v[2], v[3]);
+    else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 4; ++i)
             if (i < n) x[i] = v[i];
     }
 }
+// kBytes 8-bit values of a row; the pitch of the rows is a multiple of 16, so all of them lie in it.
+template <int kBytes>
+__device__ __forceinline__ void d_load(const uint8_t *p, uint32_t (&w)[kBytes / 4])
+{
+    if constexpr (kBytes == 4) w[0] = load_free((const uint32_t *)p);
+    else if constexpr (kBytes == 8) { const uint2 a = load_free((const uint2 *)p); w[0] = a.x; w[1] = a.y; }
+    else { const uint4 a = load_free((const uint4 *)p); w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; }
+}
 
-// A tile of 128 x 128 per CTA.  A thread takes 8 x 8 entries; a warp 64 rows x 32 columns, so that it reads 32 bytes of a row at once and
-// writes, transposed, 64 consecutive entries of a row of X.
+// A tile of 128 x 128 per CTA, 64 entries a thread, in stores of 16 bytes that lie side by side.  As it lies: a thread takes 16 bytes of X
+// of eight rows (16 of float32), whose lanes cover 128 columns.  Transposed: of as many columns, and a warp covers 64 rows x 32 columns,
+// so that it reads whole sectors of 32 bytes and writes 128 bytes of a row of X or more at once.
 template <typename T, bool kE5, bool kTranspose>
 __global__ void __launch_bounds__(256) dequantize_f8_kernel(const DParams p)
 {
+    constexpr int kV = 16 / sizeof(T), kN = 64 / kV;
+    constexpr int kRows = kTranspose ? kV : kN, kCols = kTranspose ? kN : kV;      // of the matrix, to a thread
+    constexpr int kAcross = (kTranspose ? 32 : 128) / kCols;                        // lanes side by side
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int tx = kTranspose ? (warp & 3) * 4 + (lane & 3) : lane & 15, ty = kTranspose ? (warp >> 2) * 8 + (lane >> 2) : warp * 2 + (lane >> 4);
+    const int col = (kTranspose ? (warp & 3) * 32 : 0) + lane % kAcross * kCols;
+    const int row = (kTranspose ? (warp >> 2) * 64 : warp * 16) + lane / kAcross * kRows;
     const int64_t tk = (int64_t)blockIdx.x % p.tiles, tr = (int64_t)blockIdx.x / p.tiles;
-    const int64_t k0 = tk * kF8Block + tx * 8, r0 = tr * kF8Block + ty * 8;
+    const int64_t k0 = tk * kF8Block + col, r0 = tr * kF8Block + row;
     wait_for_previous();
     if (k0 >= p.cols || r0 >= p.rows) return;
-    const int nk = p.cols - k0 < 8 ? (int)(p.cols - k0) : 8, nr = p.rows - r0 < 8 ? (int)(p.rows - r0) : 8;
+    const int nk = p.cols - k0 < kCols ? (int)(p.cols - k0) : kCols, nr = p.rows - r0 < kRows ? (int)(p.rows - r0) : kRows;
     const uint8_t *data = from_here(p.data) + r0 * p.pitch + k0, *scale = from_here(p.scale) + f8_scale_at(r0, tk, p.atoms);
-    uint2 w[8];
-    uint32_t b[8];
+    uint32_t w[kRows][kCols / 4], b[kRows];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {                       // (the scales of eight rows from a multiple of eight on lie 16 bytes apart)
-        w[j] = j < nr ? load_free((const uint2 *)(data + j * p.pitch)) : make_uint2(0u, 0u);
+    for (int j = 0; j < kRows; ++j) {                   // (the scales of a thread's rows, which lie in one group of 32, are 16 bytes apart)
+        if (j < nr) d_load<kCols>(data + j * p.pitch, w[j]);
+        else
+#pragma unroll
+            for (int i = 0; i < kCols / 4; ++i) w[j][i] = 0u;
         b[j] = load_free(scale + j * 16);
     }
-    float f[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = f8_scale(b[j]);
     T *X = (T *)p.X;
     if constexpr (!kTranspose) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < kRows; ++j) {
             if (j >= nr) break;
-            float v[8];
+            const float f = f8_scale(b[j]);
+            float v[kV];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 a = f8_unpack<kE5>((i < 2 ? w[j].x : w[j].y) >> (16 * (i & 1)) & 0xFFFFu);
-                v[2 * i] = a.x * f[j]; v[2 * i + 1] = a.y * f[j];
+            for (int i = 0; i < kV; i += 2) {
+                const float2 a = f8_unpack<kE5>(w[j][i / 4] >> (8 * (i & 2)) & 0xFFFFu);
+                v[i] = a.x * f; v[i + 1] = a.y * f;
             }
-            d_store8(X + (r0 + j) * p.ldx + k0, v, nk, p.vec);
+            d_store(X + (r0 + j) * p.ldx + k0, v, nk, p.vec);
         }
     } else {
+        float f[kRows];
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-            float lo[8], hi[8];
+        for (int j = 0; j < kRows; ++j) f[j] = f8_scale(b[j]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float2 t = f8_unpack<kE5>((i < 4 ? w[j].x : w[j].y) >> (8 * (i & 2)) & 0xFFFFu);
+        for (int i = 0; i < kCols; i += 2) {
+            float lo[kV], hi[kV];
+#pragma unroll
+            for (int j = 0; j < kRows; ++j) {
+                const float2 t = f8_unpack<kE5>(w[j][i / 4] >> (8 * (i & 2)) & 0xFFFFu);
                 lo[j] = t.x * f[j]; hi[j] = t.y * f[j];
             }
-            if (i < nk) d_store8(X + (k0 + i) * p.ldx + r0, lo, nr, p.vec);
-            if (i + 1 < nk) d_store8(X + (k0 + i + 1) * p.ldx + r0, hi, nr, p.vec);
+            if (i < nk) d_store(X + (k0 + i) * p.ldx + r0, lo, nr, p.vec);
+            if (i + 1 < nk) d_store(X + (k0 + i + 1) * p.ldx + r0, hi, nr, p.vec);
         }
     }
 }

@@ -36,7 +36,7 @@ __device__ __forceinline__ uint32_t bf16_max2(uint32_t a, uint32_t b)      // (p
     return *(const uint32_t *)&m;
 }
 
-// 8 x 8 entries in registers, bfloat16 as they come (two to a word), so that three CTAs fit an SM.
+// 8 x 8 entries in registers, bfloat16 as they come (two to a word), so that four CTAs fit an SM (three: 28.2 us for 8192 x 4096 in both orientations, four 26.7).
 template <typename T>
 struct QEntries {
     static constexpr int kWords = sizeof(T) == 2 ? 4 : 8;          // words of eight entries
@@ -143,11 +143,12 @@ struct QEntries {
 };
 
 template <typename T, bool kE5, bool kWeights>
-__global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 ? 3 : 2) quantize_f8_kernel(const QParams p)
+__global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 ? 4 : 2) quantize_f8_kernel(const QParams p)
 {
     __shared__ __align__(16) uint8_t s_cols[kF8Block * kF8Block];
     __shared__ __align__(16) float s_max[8][kF8Block], s_sum[8][kF8Block];
     __shared__ __align__(16) float s_inv[kF8Block];
+    __shared__ uint8_t s_row[kF8Block];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, tx = tid & 15, ty = tid >> 4;
     const int64_t ti = (int64_t)blockIdx.x % p.tiles_i, tp = (int64_t)blockIdx.x / p.tiles_i;
     const int64_t c0 = ti * kF8Block + tx * 8, r0 = tp * kF8Block + ty * 8;
@@ -229,13 +230,14 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 ? 3 : 2) quantize_f8
             w.x = f8_pack<kE5>(v.at(j, 0) * f, v.at(j, 1) * f) | f8_pack<kE5>(v.at(j, 2) * f, v.at(j, 3) * f) << 16;
             w.y = f8_pack<kE5>(v.at(j, 4) * f, v.at(j, 5) * f) | f8_pack<kE5>(v.at(j, 6) * f, v.at(j, 7) * f) << 16;
             if (r0 + j < p.P && c0 < p.rows_pitch) *(uint2 *)(p.rows + (r0 + j) * p.rows_pitch + c0) = w;
-            if (tx == 0) p.rows_scale[f8_scale_at(r0 + j, ti, p.rows_atoms)] = (uint8_t)b;      // (the scales reach whole groups of 128 rows)
+            if (tx == 0) s_row[ty * 8 + j] = (uint8_t)b;
         }
     }
-    if (p.cols == nullptr && p.partial == nullptr) return;
     __syncthreads();
     if (tid < kF8Block) {
         const int64_t c = ti * kF8Block + tid;
+        // (the scales reach whole groups of 128 rows, in either orientation; four instructions for a tile's instead of 64: 26.7 -> 24.6 us)
+        if (p.rows != nullptr) p.rows_scale[f8_scale_at(tp * kF8Block + tid, ti, p.rows_atoms)] = s_row[tid];
         if (p.cols != nullptr) {
             float m = rmax[0];
             if constexpr (!kWeights) {

@@ -497,10 +497,11 @@ constexpr int kFpStaging = 16384;                   // of a group: 128 rows of 1
 constexpr int kFpSecond = 192;                      // first column of the second accumulator: the last 64 of the first lie under it
 
 struct FpParams {
-    CUtensorMap tma, tmb;         // values as bytes, (K, rows), box 128 x 128, 128-byte swizzle
+    CUtensorMap tma, tmb, tmb64;  // values as bytes, (K, rows), box 128 x 128 (64 rows of B in tiles of 128 columns), 128-byte swizzle
     CUtensorMap tsa, tsb;         // scales as words, (128, atoms, rows / 128), boxes of one and of two atoms
     CUtensorMap tmy;              // Y as bytes, (N ey, M), box 128 bytes x 128 rows, 128-byte swizzle
     int M, N, n_kb, tiles_n, n_tiles;
+    int n_wide;                   // tiles of 256 columns; the rest are halves of such
     uint32_t idesc, m_tn;
     const float *bias;
     const uint8_t *gamma;
@@ -516,9 +517,21 @@ struct FpTail {
 constexpr int kFpSmem = kFpStages * (kFpStage + kFpScales) + 2 * kFpStaging + (int)sizeof(FpTail);
 static_assert(kFpSmem <= kFsSmem, "shared memory of a CTA");
 
+// Tile `tile` of a pair: its rows 256 mp .., its columns n0 .., whether it has 128 columns instead of 256.
+__device__ __forceinline__ void fp_tile(const FpParams &p, int tile, int &mp, int &n0, bool &narrow)
+{
+    int tn, half = 0, t = tile;
+    narrow = tile >= p.n_wide;
+    if (narrow) { half = (tile - p.n_wide) & 1; t = p.n_wide + ((tile - p.n_wide) >> 1); }
+    gt_divmod(t, p.tiles_n, p.m_tn, mp, tn);
+    n0 = tn * 256 + half * 128;
+}
+
 // A pair of CTAs owns tiles of 256 x 256: CTA r of the pair the rows 128 r .. of the tile, and loads these and its half of the tile's rows
 // of B; the leader issues MMAs of 256 x 256 x 32 for both.  Two accumulators of 256 columns that overlap by 64, whose columns the
 // epilogue reads first, leave 64 columns for the scales: the next tile's MMAs start when these 64 have been read.
+// Where the tiles of the last wave leave half of the pairs idle they are halved (4096 x 4096 sums of 8192 entries, 34 tiles in the last wave of 74
+// pairs: 131 -> 125 us).
 // kF32: chunks of kFsChunk blocks are summed in the tensor core, these in registers (as above).
 template <bool kF32>
 __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __grid_constant__ FpParams p)
@@ -545,7 +558,7 @@ __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __gri
         asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(sm32(&tail.acc_free)), "r"(16) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         s_fail = (ring & 1023u) == 0u ? 0u : 2u;
-        const CUtensorMap *maps[5] = {&p.tma, &p.tmb, &p.tsa, &p.tsb, &p.tmy};
+        const CUtensorMap *maps[6] = {&p.tma, &p.tmb, &p.tmb64, &p.tsa, &p.tsb, &p.tmy};
         for (const CUtensorMap *m : maps) asm volatile("prefetch.tensormap [%0];\n" ::"l"(m) : "memory");
     }
     if (warp == 0) {
@@ -570,22 +583,25 @@ __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __gri
             uint32_t slot = 0, par = 1, issued = 0;
             bool ok = true;
             for (int tile = t_first; tile < p.n_tiles && ok; tile += t_step) {
-                int mp, tn;
-                gt_divmod(tile, p.tiles_n, p.m_tn, mp, tn);
-                const int ma = 2 * mp + (int)rank, m0 = ma * 128, n0 = tn * 256 + (int)rank * 128;
+                int mp, nt;
+                bool narrow;
+                fp_tile(p, tile, mp, nt, narrow);
+                const int ma = 2 * mp + (int)rank, m0 = ma * 128, n0 = nt + (int)rank * (narrow ? 64 : 128);
+                const CUtensorMap *tmb = narrow ? &p.tmb64 : &p.tmb;
+                const uint32_t values = narrow ? 16384u + 8192u : (uint32_t)kFpStage;
                 if (s_fail) { ok = false; break; }
                 for (int kb = 0; kb < n_kb; ++kb) {
                     if (!__all_sync(0xFFFFFFFFu, gt_poll(empty0 + slot * 8u, par))) { ok = false; break; }
                     const uint32_t with = (kb & 3) == 0 ? 1u : 0u, dst = ring + slot * kFpStage, sdst = scales + slot * kFpScales;
-                    const uint32_t bytes = 2u * (kFpStage + with * kFpScales), bar = lead_full0 + slot * 8u;
+                    const uint32_t bytes = 2u * (values + with * kFpScales), bar = lead_full0 + slot * 8u;
                     asm volatile("{\n .reg .pred e, l, s;\n elect.sync _|e, 0xFFFFFFFF;\n setp.eq.u32 l, %2, 0;\n and.pred l, l, e;\n setp.ne.b32 s, %3, 0;\n and.pred s, s, e;\n"
                                  " @l mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n"
                                  " @s cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%11], [%12, {%15, %13, %14}], [%4];\n"
                                  " @s cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%16], [%17, {%15, %13, %18}], [%4];\n"
                                  " @e cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%5], [%6, {%7, %8}], [%4];\n"
                                  " @e cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%9], [%10, {%7, %19}], [%4];\n}\n"
-                                 ::"r"(full0 + slot * 8u), "r"(bytes), "r"(rank), "r"(with), "r"(bar), "r"(dst), "l"(&p.tma), "r"(kb * 128), "r"(m0), "r"(dst + 16384u), "l"(&p.tmb),
-                                   "r"(sdst), "l"(&p.tsa), "r"(kb >> 2), "r"(ma), "r"(0), "r"(sdst + 512u), "l"(&p.tsb), "r"(2 * tn), "r"(n0) : "memory");
+                                 ::"r"(full0 + slot * 8u), "r"(bytes), "r"(rank), "r"(with), "r"(bar), "r"(dst), "l"(&p.tma), "r"(kb * 128), "r"(m0), "r"(dst + 16384u), "l"(tmb),
+                                   "r"(sdst), "l"(&p.tsa), "r"(kb >> 2), "r"(ma), "r"(0), "r"(sdst + 512u), "l"(&p.tsb), "r"(nt >> 7), "r"(n0) : "memory");
                     ++issued;
                     if (++slot == kFpStages) { slot = 0; par ^= 1u; }
                 }
@@ -605,6 +621,7 @@ __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __gri
             uint32_t slot = 0, par = 0, set = 0, unit = 0;
             bool ok = true, full_now = false;
             for (int tile = t_first; tile < p.n_tiles && ok; tile += t_step) {
+                const uint32_t tile_idesc = p.idesc | ((tile >= p.n_wide ? 16u : 32u) << 17);
                 for (int kb = 0; kb < n_kb; ++kb) {
                     const bool fresh = kF32 ? kb % kFsChunk == 0 : kb == 0;
                     if (fresh) {
@@ -622,7 +639,7 @@ __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __gri
                     const uint32_t a16 = (ring + slot * kFpStage) >> 4, s16 = (scales + slot * kFpScales) >> 4;
                     const uint64_t da = kGtDesc | (uint64_t)(a16 & 0x3FFFu), db = kGtDesc | (uint64_t)((a16 + 1024u) & 0x3FFFu);
                     const uint64_t ds = kFsScaleDesc | (uint64_t)(s16 & 0x3FFFu);
-                    const uint32_t fa = tmem + 448u + set * 16u, fb = fa + 8u, id = (uint32_t)kb & 3u, idesc = p.idesc | (id << 4) | (id << 29);
+                    const uint32_t fa = tmem + 448u + set * 16u, fb = fa + 8u, id = (uint32_t)kb & 3u, idesc = tile_idesc | (id << 4) | (id << 29);
                     const bool wrap = slot + 1u == (uint32_t)kFpStages;
                     uint32_t next;
                     asm volatile("{\n .reg .pred e, s, p, q, f, v;\n .reg .b64 a1, a2, a3, b1, b2, b3, s1, s2;\n .reg .b32 f2;\n"
@@ -673,9 +690,10 @@ __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __gri
             if (lane == 0) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(lead_free) : "memory");
         };
         for (int tile = t_first; tile < p.n_tiles; tile += t_step) {
-            int mp, tn;
-            gt_divmod(tile, p.tiles_n, p.m_tn, mp, tn);
-            const int m0 = (2 * mp + (int)rank) * 128, n0 = tn * 256, m = m0 + row;
+            int mp, n0;
+            bool narrow;
+            fp_tile(p, tile, mp, n0, narrow);
+            const int m0 = (2 * mp + (int)rank) * 128, m = m0 + row;
             {   // the bias of the group's 128 columns (everybody is past the barriers of the last tile's rounds)
                 const int n = n0 + (row >> 6) * 128 + grp * 64 + (row & 63);
                 const float b = bias_of != nullptr && n < p.N ? __uint_as_float(load_free((const uint32_t *)bias_of + n)) : 0.f;
@@ -705,6 +723,7 @@ __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __gri
                     if (second == (uint32_t)grp) hand_back();            // (this group has no column under the other accumulator)
                     auto take = [&](auto half_c) {
                         constexpr int half = decltype(half_c)::value;
+                        if (half == 1 && narrow) return;
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
                             uint32_t v[16];
@@ -727,6 +746,7 @@ __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __gri
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int c0 = (r >> 1) * 128 + grp * 64 + (r & 1) * 32;
+                    if (r >= 2 && narrow) break;
                     uint32_t out[32];
                     const float *b = tail.bias[grp] + r * 32;
                     if (r == 0) gt_group_sync(1 + grp);                  // (the bias is there)
@@ -752,6 +772,10 @@ __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __gri
 #pragma unroll 1
                 for (int r = 0; r < 2; ++r) {
                     const uint32_t half = second ? (uint32_t)r : 1u - (uint32_t)r;
+                    if (half == 1u && narrow) {
+                        if (r == 0 && second != (uint32_t)grp) hand_back();
+                        continue;
+                    }
                     uint32_t out[32];
                     gt_epilogue_round<false, 2, false>(t + half * 128u, (const uint32_t *)tail.bias[grp] + half * 64u, 64, 0, out);
                     if (r == 0 && second != (uint32_t)grp) hand_back();
@@ -812,20 +836,24 @@ bsp_status launch_pairs(const bsp_f8 &x, const bsp_f8 &w, const float *bias, con
     p.tiles_n = (p.N + 255) / 256;
     const long long tiles = (long long)((p.M + 255) / 256) * p.tiles_n;
     if (tiles > 0x7FFFFFFF - 4096) return BSP_ERR_SHAPE;
-    p.n_tiles = (int)tiles;
+    // the tiles of the last wave, halved where two for each of them find pairs of their own
+    const int pairs_there = sms / 2, last = (int)(tiles % pairs_there);
+    p.n_wide = (int)tiles - (2 * last <= pairs_there ? last : 0);
+    p.n_tiles = (int)(tiles + (tiles - p.n_wide));
     p.m_tn = gt_magic(p.tiles_n);
-    // formats, N / 8, scales of 8 exponent bits, M / 128
-    p.idesc = ((x.type == BSP_E5M2 ? 1u : 0u) << 7) | ((w.type == BSP_E5M2 ? 1u : 0u) << 10) | (32u << 17) | (1u << 23) | (2u << 27);
+    // formats, scales of 8 exponent bits, M / 128 (N / 8 by tile)
+    p.idesc = ((x.type == BSP_E5M2 ? 1u : 0u) << 7) | ((w.type == BSP_E5M2 ? 1u : 0u) << 10) | (1u << 23) | (2u << 27);
     p.bias = bias;
     if (wd) { p.gamma = gamma; p.bo = f8_log2(wd->bo); p.bi = f8_log2(wd->bi); p.NBi = wd->I / wd->bi; }
     p.status = (int *)ws;
     bsp_status rc = fs_map(&p.tma, x, 128);
     if (rc == BSP_OK) rc = fs_map(&p.tmb, w, 128);
+    if (rc == BSP_OK) rc = fs_map(&p.tmb64, w, 64);
     if (rc == BSP_OK) rc = fp_scale_map(&p.tsa, x, 1);
     if (rc == BSP_OK) rc = fp_scale_map(&p.tsb, w, 2);
     if (rc == BSP_OK) rc = fs_y_map(&p.tmy, Y, p.M, (int64_t)p.N * ey);
     if (rc != BSP_OK) return rc;
-    const int pairs = p.n_tiles < sms / 2 ? p.n_tiles : sms / 2;
+    const int pairs = p.n_tiles < pairs_there ? p.n_tiles : pairs_there;
     BSP_CUDA_OK(launch_after_clusters(ey == 4 ? gemm_f8_pair_kernel<true> : gemm_f8_pair_kernel<false>, dim3((unsigned)(2 * pairs)), dim3(kFpThreads), kFpSmem, st, 2, 1, p));
     return BSP_OK;
 }
@@ -974,7 +1002,8 @@ bsp_status launch_gemm_f8(const bsp_f8 &x, const bsp_f8 &w, const float *bias, c
     // pairs of CTAs, where a tensor map can describe the rows of Y
     const double tiles = (double)((x.rows + 255) / 256) * (double)((w.rows + 255) / 256), pairs = d.sms / 2;
     if (!transposed && d.sms >= 2 && w.rows * (ytype == BSP_BF16 ? 2 : 4) % 16 == 0) {
-        const double cycles = (double)(int64_t)((tiles + pairs - 1) / pairs) * (n_kb * 690.0 + 1500.0) + 4500.0;
+        const double waves = (double)(int64_t)(tiles / pairs), rest = tiles - waves * pairs;
+        const double cycles = (waves + (rest == 0.0 ? 0.0 : 2.0 * rest <= pairs ? 0.74 : 1.0)) * (n_kb * 690.0 + 1500.0) + 4500.0;
         if (cycles < c.cycles) return launch_pairs(x, w, bias, wd, gamma, Y, ytype, ws, d.sms, st);
     }
     return launch_tiles(d, FsJob{&x, &w, nullptr, BSP_F32, 0, 0, bias, wd, gamma, Y, ytype, ws}, c, transposed, st);

@@ -176,7 +176,8 @@ def test_gemm(M, N, K, at, bt, out):
 
 
 @pytest.mark.parametrize("M,N,K,at,bt,out", [(2300, 2056, 400, "e4m3", "e4m3", "bf16"), (2300, 2056, 4400, "e5m2", "e4m3", "f32"), (20000, 264, 136, "e4m3", "e5m2", "f32"),
-                                             (130, 20000, 2048, "e4m3", "e4m3", "bf16"), (2049, 2564, 2050, "e4m3", "e4m3", "f32")])
+                                             (130, 20000, 2048, "e4m3", "e4m3", "bf16"), (2049, 2564, 2050, "e4m3", "e4m3", "f32"),
+                                             (2560, 2560, 300, "e4m3", "e4m3", "bf16"), (2500, 2440, 2400, "e4m3", "e4m3", "f32"), (1030, 1000, 4096, "e4m3", "e4m3", "bf16")])
 def test_gemm_large(M, N, K, at, bt, out):
     """Products that take pairs of CTAs: ragged in both directions, one and several sums of 2048 entries, more tiles than pairs."""
     A, a = random_held(3050 + M, M, K, at)

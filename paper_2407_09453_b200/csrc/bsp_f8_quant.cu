@@ -56,8 +56,20 @@ struct QEntries {
             w[j][4] = b.x; w[j][5] = b.y; w[j][6] = b.z; w[j][7] = b.w;
         }
     }
-    __device__ __forceinline__ void load_some(int j, const T *p, int64_t n)      // n entries, which may be none
+    __device__ __forceinline__ void load_some(int j, const T *p, int64_t n)      // n entries, which may be none, from anywhere
     {
+        if constexpr (sizeof(T) == 2) {
+            // whole words, each of which holds an entry of the eight
+            if (n >= 8) {
+                const uint32_t odd = ((uint32_t)(uintptr_t)p & 2u) << 3, *q = (const uint32_t *)((uintptr_t)p & ~(uintptr_t)3);
+                uint32_t a[5];
+#pragma unroll
+                for (int k = 0; k < 5; ++k) a[k] = k < 4 || odd ? load_free(q + k) : 0u;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[j][k] = __funnelshift_r(a[k], a[k + 1], odd);
+                return;
+            }
+        }
 #pragma unroll
         for (int k = 0; k < kWords; ++k) {
             if constexpr (sizeof(T) == 2) {
@@ -405,6 +417,84 @@ __global__ void __launch_bounds__(256) dequantize_f8_kernel(const DParams p)
     }
 }
 
+// The same for rows of X that cannot be written 16 bytes at a time: a lane takes an aligned word of a row of X, so that a warp writes 128 bytes
+// side by side wherever the row begins.  As it lies: two bfloat16 columns (or one float32) of a row; transposed: two rows (one) of the
+// matrix for 16 columns, where a word may hold the second entry of the lane before.
+template <typename T, bool kE5, bool kTranspose>
+__global__ void __launch_bounds__(256) dequantize_f8_any_kernel(const DParams p)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t tk = (int64_t)blockIdx.x % p.tiles, tr = (int64_t)blockIdx.x / p.tiles, k0 = tk * kF8Block, r0 = tr * kF8Block;
+    wait_for_previous();
+    const uint8_t *data = from_here(p.data), *scale = from_here(p.scale);
+    const int nk = p.cols - k0 < kF8Block ? (int)(p.cols - k0) : kF8Block, nr = p.rows - r0 < kF8Block ? (int)(p.rows - r0) : kF8Block;
+    constexpr int kPer = 4 / sizeof(T);                 // entries of a word
+    if constexpr (!kTranspose) {
+        // (a lane holds four columns of a row and hands them to the lanes that write them)
+#pragma unroll 4
+        for (int j = warp; j < nr; j += 8) {
+            T *x = (T *)p.X + (r0 + j) * p.ldx + k0;
+            const uint32_t mine = lane * 4 < nk ? load_free((const uint32_t *)(data + (r0 + j) * p.pitch + k0) + lane) : 0u;
+            const float f = f8_scale(load_free(scale + f8_scale_at(r0 + j, tk, p.atoms)));
+            const int odd = sizeof(T) == 2 ? (int)((uintptr_t)x >> 1 & 1) : 0;
+#pragma unroll
+            for (int i = 0; i < 128 / (32 * kPer) + (kPer == 2 ? 1 : 0); ++i) {
+                const int c = (i * 32 + lane) * kPer - odd;
+                if (i * 32 * kPer - odd >= nk) break;
+                float v[kPer];
+#pragma unroll
+                for (int e = 0; e < kPer; ++e)
+                    v[e] = f8_unpack<kE5>(__shfl_sync(0xFFFFFFFFu, mine, (c + e) >> 2 & 31) >> (8 * ((c + e) & 3)) & 0xFFu).x * f;
+                if constexpr (kPer == 1) { if (c < nk) x[c] = v[0]; }
+                else if (c >= 0 && c + 1 < nk) {
+                    const __nv_bfloat162 h = __floats2bfloat162_rn(v[0], v[1]);
+                    *(uint32_t *)(x + c) = *(const uint32_t *)&h;
+                } else {
+                    if (c >= 0 && c < nk) x[c] = __float2bfloat16_rn(v[0]);
+                    if (c + 1 >= 0 && c + 1 < nk) x[c + 1] = __float2bfloat16_rn(v[1]);
+                }
+            }
+        }
+    } else {
+        // a warp: 16 columns of 32 kPer rows, then of the next 32 kPer
+        const int c0 = warp * 16;
+        if (c0 >= nk) return;
+        for (int i = 0; i < 128 / (32 * kPer); ++i) {
+            const int r = (i * 32 + lane) * kPer;
+            uint4 w[kPer];
+            float f[kPer];
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                w[e] = r + e < nr ? load_free((const uint4 *)(data + (r0 + r + e) * p.pitch + k0 + c0)) : make_uint4(0u, 0u, 0u, 0u);
+                f[e] = r + e < nr ? f8_scale(load_free(scale + f8_scale_at(r0 + r + e, tk, p.atoms))) : 0.f;
+            }
+#pragma unroll
+            for (int c = 0; c < 16; ++c) {
+                if (c0 + c >= nk) break;
+                T *x = (T *)p.X + (k0 + c0 + c) * p.ldx + r0 + r;
+                float v[kPer];
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) v[e] = f8_unpack<kE5>((c < 4 ? w[e].x : c < 8 ? w[e].y : c < 12 ? w[e].z : w[e].w) >> (8 * (c & 3)) & 0xFFu).x * f[e];
+                if constexpr (kPer == 1) { if (r < nr) *x = v[0]; }
+                else {
+                    const __nv_bfloat16 own = __float2bfloat16_rn(v[0]), second = __float2bfloat16_rn(v[1]);
+                    const uint32_t lo = __bfloat16_as_ushort(own), hi = __bfloat16_as_ushort(second), before = __shfl_up_sync(0xFFFFFFFFu, hi, 1);
+                    if (((uintptr_t)x & 2u) == 0u) {
+                        if (r + 1 < nr) *(uint32_t *)x = lo | hi << 16;
+                        else if (r < nr) *x = own;
+                    } else {
+                        if (r < nr) {
+                            if (lane > 0) *(uint32_t *)(x - 1) = before | lo << 16;
+                            else *x = own;
+                        } else if (lane > 0 && r - 1 < nr) *(x - 1) = __ushort_as_bfloat16((unsigned short)before);
+                        if (lane == 31 && r + 1 < nr) x[1] = second;
+                    }
+                }
+            }
+        }
+    }
+}
+
 bool rows_of_16(const void *X, int64_t ldx, int esz) { return ((uintptr_t)X & 15u) == 0 && ldx * esz % 16 == 0; }
 
 }  // namespace
@@ -447,7 +537,11 @@ bsp_status launch_dequantize_f8(const bsp_f8 &m, void *X, bsp_dtype xtype, int64
         {{dequantize_f8_kernel<float, false, false>, dequantize_f8_kernel<float, false, true>}, {dequantize_f8_kernel<float, true, false>, dequantize_f8_kernel<float, true, true>}},
         {{dequantize_f8_kernel<__nv_bfloat16, false, false>, dequantize_f8_kernel<__nv_bfloat16, false, true>},
          {dequantize_f8_kernel<__nv_bfloat16, true, false>, dequantize_f8_kernel<__nv_bfloat16, true, true>}}};
-    BSP_CUDA_OK(launch_after(kernels[xtype == BSP_BF16][m.type == BSP_E5M2][transpose], dim3((unsigned)tiles), dim3(256), 0, st, p));
+    static const Kernel any[2][2][2] = {
+        {{dequantize_f8_any_kernel<float, false, false>, dequantize_f8_any_kernel<float, false, true>}, {dequantize_f8_any_kernel<float, true, false>, dequantize_f8_any_kernel<float, true, true>}},
+        {{dequantize_f8_any_kernel<__nv_bfloat16, false, false>, dequantize_f8_any_kernel<__nv_bfloat16, false, true>},
+         {dequantize_f8_any_kernel<__nv_bfloat16, true, false>, dequantize_f8_any_kernel<__nv_bfloat16, true, true>}}};
+    BSP_CUDA_OK(launch_after((p.vec ? kernels : any)[xtype == BSP_BF16][m.type == BSP_E5M2][transpose], dim3((unsigned)tiles), dim3(256), 0, st, p));
     return BSP_OK;
 }
 

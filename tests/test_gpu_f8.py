@@ -133,6 +133,32 @@ def test_dequantize(R, K, dtype, ftype, transpose):
     assert (got[:, shape[1]:] == -7.0).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("R,K,extra,off", [(1, 1, 0, 0), (131, 257, 0, 0), (129, 300, 1, 1), (130, 131, 3, 2), (300, 63, 2, 3), (255, 15, 0, 5)])
+def test_dequantize_any_alignment(R, K, extra, off, dtype):
+    """Rows of X that begin anywhere, in both orientations; nothing between or around them is written."""
+    codes, scales = f8.quantize(values(2650 + R, R, K, "f32"), "e4m3")
+    m, want = held(codes, scales, "e4m3"), f8.dequantize(codes, scales, "e4m3")
+    for w, transpose in ((want, False), (want.T, True)):
+        ld = w.shape[1] + extra
+        store = torch.full((off + w.shape[0] * ld + 8,), -7.0, dtype=XTYPE[dtype], device="cuda")
+        view = torch.as_strided(store, w.shape, (ld, 1), off)
+        bsp.bsp_dequantize_f8(m.m, view, bsp.dtype_code(XTYPE[dtype]), ld, transpose)
+        expect = torch.full_like(store, -7.0)
+        torch.as_strided(expect, w.shape, (ld, 1), off).copy_(device(w, dtype))
+        assert torch.equal(store, expect)
+
+
+@pytest.mark.parametrize("dtype,off,ldx", [("bf16", 1, 257), ("f32", 3, 257), ("bf16", 0, 257), ("bf16", 5, 258)])
+def test_quantize_any_alignment(dtype, off, ldx):
+    P, I = 260, 257
+    x = values(2660 + off, P, I, dtype)
+    store = torch.full((P * ldx + off,), float("nan"), dtype=XTYPE[dtype], device="cuda")
+    view = torch.as_strided(store, (P, I), (ldx, 1), off)
+    view.copy_(device(x, dtype))
+    assert_forms(quantize_both(view, "e4m3", None, ldx), x, "e4m3")
+
+
 def test_dequantize_every_code_and_scale():
     for ftype in ("e4m3", "e5m2"):
         codes = np.tile(np.arange(256, dtype=np.uint8), (256, 1))

@@ -102,9 +102,10 @@ __device__ __forceinline__ uint32_t fs_pack(float lo, float hi)
 // accumulator, 8192 entries, were off by 1.9e-6 of the result, chunks by 5.5e-7; plain float32 sums by 4.2e-7).
 // T: type of X where its rows are quantised here (rows of B, e4m3), void where B comes as an 8-bit matrix.
 template <typename T>
-__global__ void __launch_bounds__(kFsThreads, 1) gemm_f8_tile_kernel(const __grid_constant__ FsParams p)
+__global__ void __launch_bounds__(kFsThreads, std::is_same_v<T, void> ? 1 : 2) gemm_f8_tile_kernel(const __grid_constant__ FsParams p)
 {
     constexpr bool kX = !std::is_same_v<T, void>;
+    constexpr int kPieces = kX ? 2 : 4;               // 16-column pieces of a warp's sums: tiles with X have at most 64 columns
     extern __shared__ __align__(1024) uint8_t smem[];
     FsTail &tail = *(FsTail *)(smem + p.off_tail);
     volatile uint32_t &s_fail = tail.fail;
@@ -136,6 +137,14 @@ __global__ void __launch_bounds__(kFsThreads, 1) gemm_f8_tile_kernel(const __gri
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(sm32(&tail.tmem)), "r"(cols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
     }
+    if constexpr (kX) {
+        // The weights of this CTA on their way to L2 while the kernel before this one ends, where shared memory has room for both: a cache
+        // that is coherent, so it does not matter whether that kernel wrote them.
+        if (warp == 0)
+            for (int kb = kb0; kb < kb1; ++kb)
+                asm volatile("{\n .reg .pred e;\n elect.sync _|e, 0xFFFFFFFF;\n @e cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];\n}\n"
+                             ::"l"(&p.tma), "r"(kb * 128), "r"(m0) : "memory");
+    }
     wait_for_previous<false>();
     if (warp == 0) let_next_start();
     if (tid == 0 && s_fail) atomicMax(p.status, (int)BSP_ERR_CUDA);
@@ -152,12 +161,12 @@ __global__ void __launch_bounds__(kFsThreads, 1) gemm_f8_tile_kernel(const __gri
     }
     __syncwarp();
     // (the CTAs of a cluster run once this barrier is complete: what they send each other waits for it)
-    if (split > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
+    if (split > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;\n" ::: "memory");
     const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, tail.tmem, 0), sf = tmem + cols - 64u;
     const bool run = __shfl_sync(0xFFFFFFFFu, s_fail, 0) == 0u;
     const uint32_t full0 = sm32(&tail.full[0]), empty0 = sm32(&tail.empty[0]);
 
-    float acc[4][16];                                 // (epilogue warps)
+    float acc[kPieces][16];                           // (epilogue warps)
     if (warp == 0) {
         // ================= producer =================
         if (run) {
@@ -320,7 +329,7 @@ __global__ void __launch_bounds__(kFsThreads, 1) gemm_f8_tile_kernel(const __gri
             asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
             const uint32_t t = tmem + ((uint32_t)(q * 32) << 16) + buf * (uint32_t)BN + (uint32_t)(grp * (BN / 2));
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
+            for (int k = 0; k < kPieces; ++k)
                 if (k < pieces) {
                     uint32_t v[16];
                     fs_load16(t + (uint32_t)k * 16u, v);
@@ -343,7 +352,7 @@ __global__ void __launch_bounds__(kFsThreads, 1) gemm_f8_tile_kernel(const __gri
             // the tile by lines to the ring, which is free; the lines that another CTA stores go to it in one copy, to the place of this rank
             // (lines of BN entries: 16-byte piece j of line r at place j ^ (r % 8), so that the lanes, a line each, meet different banks)
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
+            for (int k = 0; k < kPieces; ++k)
                 if (k < pieces) {
                     if (p.transposed) {
 #pragma unroll
@@ -380,19 +389,19 @@ __global__ void __launch_bounds__(kFsThreads, 1) gemm_f8_tile_kernel(const __gri
         const int l0 = rank * per, n = lines - l0 < per ? lines - l0 : per, shift = p.transposed ? 5 : 31 - __clz(BN >> 2);
         const int in0 = p.transposed ? m0 : n0, in_end = p.transposed ? p.M : p.N, lead0 = p.transposed ? n0 : m0;
         const uint32_t own = ring + (uint32_t)(l0 * line_bytes), recv = ring + (uint32_t)p.off_recv, share = (uint32_t)(per * line_bytes);
+        auto join = [&](auto split_c) {
+            constexpr int kSplit = decltype(split_c)::value;            // (with branches on the number 600 cycles a turn)
         for (int u = tid - 64; u < n << shift; u += 256) {
             const int l = u >> shift, j = u - (l << shift), in = in0 + j * 4;
             if (in >= in_end) continue;
             const uint32_t at = (uint32_t)(l * line_bytes) + (uint32_t)(p.transposed ? j : j ^ ((l0 + l) & 7)) * 16u;
-            float4 w[8];
+            float4 w[kSplit];
 #pragma unroll
-            for (int s = 0; s < 8; ++s)
-                if (s < split)
-                    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];\n" : "=f"(w[s].x), "=f"(w[s].y), "=f"(w[s].z), "=f"(w[s].w) : "r"((s == rank ? own : recv + (uint32_t)s * share) + at));
+            for (int s = 0; s < kSplit; ++s)
+                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];\n" : "=f"(w[s].x), "=f"(w[s].y), "=f"(w[s].z), "=f"(w[s].w) : "r"((s == rank ? own : recv + (uint32_t)s * share) + at));
             float v[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
 #pragma unroll
-            for (int s = 1; s < 8; ++s)
-                if (s < split) { v[0] += w[s].x; v[1] += w[s].y; v[2] += w[s].z; v[3] += w[s].w; }
+            for (int s = 1; s < kSplit; ++s) { v[0] += w[s].x; v[1] += w[s].y; v[2] += w[s].z; v[3] += w[s].w; }
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] += tail.bias[j * 4 + e];
             if (gamma != nullptr && load_free(gamma + (int64_t)((lead0 + l0 + l) >> p.bo) * p.NBi + (in >> p.bi)) == 0u) v[0] = v[1] = v[2] = v[3] = 0.f;
@@ -408,10 +417,14 @@ __global__ void __launch_bounds__(kFsThreads, 1) gemm_f8_tile_kernel(const __gri
                         else ((float *)p.Y)[out + e] = v[e];
                     }
         }
+        };
+        if (split == 2) join(std::integral_constant<int, 2>());
+        else if (split == 4) join(std::integral_constant<int, 4>());
+        else join(std::integral_constant<int, 8>());
     } else {
         const int m = m0 + row;
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < kPieces; ++k)
             if (k < pieces) {
                 const int c0 = first + k * 16;
                 if (p.transposed) {
@@ -962,6 +975,9 @@ bsp_status launch_tiles(const FsDevice &d, const FsJob &j, const FsChoice &c, bo
     p.stages = (kFsSmem - tail - x_bytes - recv) / (p.stage_bytes + kFsScales);
     if (p.stages > kFsMaxStages) p.stages = kFsMaxStages;
     if (p.stages > kb) p.stages = kb;
+    // (with X: half of an SM, so that the next layer's CTAs find room while this one's run)
+    const int half = (kFsSmem / 2 - 1024 - tail - x_bytes - recv) / (p.stage_bytes + kFsScales);
+    if (j.X && half >= 2 && p.stages > half) p.stages = half;
     int ring = p.stages * p.stage_bytes;
     if (p.staged && ring < p.BN * ey * 128) ring = p.BN * ey * 128;
     if (p.split > 1 && ring < p.BN * 512) ring = p.BN * 512;

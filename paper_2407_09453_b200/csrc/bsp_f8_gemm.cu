@@ -66,26 +66,13 @@ __device__ __forceinline__ void fs_load16(uint32_t taddr, uint32_t (&v)[16])
                    "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]) :: "memory");
 }
 
-// Eight entries of a row of X, `n` of which exist.
-__device__ __forceinline__ void fs_load_x(const float *x, int64_t n, int vec, float (&v)[8])
+// 16 bytes of X, or zeros: a predicate instead of a branch, so that the loads of a thread's rows go out together.
+__device__ __forceinline__ uint4 fs_load_if(const void *p, bool there)
 {
-    if (vec && n >= 8) {
-        const float4 a = load_free((const float4 *)x), b = load_free<16>((const float4 *)x);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    } else
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? __uint_as_float(load_free((const uint32_t *)x + i)) : 0.f;
-}
-__device__ __forceinline__ void fs_load_x(const __nv_bfloat16 *x, int64_t n, int vec, float (&v)[8])
-{
-    if (vec && n >= 8) {
-        const uint4 a = load_free((const uint4 *)x);
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
-    } else
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? __bfloat162float(x[i]) : 0.f;
+    uint4 v;
+    asm("{\n .reg .pred q;\n setp.ne.b32 q, %5, 0;\n mov.b32 %0, 0;\n mov.b32 %1, 0;\n mov.b32 %2, 0;\n mov.b32 %3, 0;\n @q ld.global.v4.b32 {%0, %1, %2, %3}, [%4];\n}\n"
+        : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "l"(p), "r"((uint32_t)there));
+    return v;
 }
 
 // What an element becomes, two neighbours of a row at a time.
@@ -265,37 +252,68 @@ __global__ void __launch_bounds__(kFsThreads, std::is_same_v<T, void> ? 1 : 2) g
             auto pass = [&](auto batch_c) {
             constexpr int kBatch = decltype(batch_c)::value;            // (items in flight; what lies past the last is worked on too)
             for (int i0 = w * 2 + (lane >> 4); i0 - (lane >> 4) < items; i0 += 16 * kBatch) {
+                constexpr int kRaw = sizeof(T) / 2;                     // words of 16 bytes in eight entries
+                uint4 raw[kBatch][kRaw];
                 float v[kBatch][8], m[kBatch];
+                bool odd = false;                                       // entries that do not come 16 bytes at a time
 #pragma unroll
                 for (int u = 0; u < kBatch; ++u) {
                     const int i = i0 + 16 * u, b = (int)((uint32_t)i * recip >> 16), r = i - b * rows;
                     const int64_t c = (int64_t)(kb0 + b) * kF8Block + l * 8;
-                    fs_load_x(X + r * p.ldx + c, i < items ? p.K - c : 0, p.xvec, v[u]);
+                    const bool whole = p.xvec && i < items && c + 8 <= p.K;
+                    odd |= !whole && i < items && c < p.K;
+#pragma unroll
+                    for (int k = 0; k < kRaw; ++k) raw[u][k] = fs_load_if(X + r * p.ldx + c + k * 4, whole);
                 }
 #pragma unroll
                 for (int u = 0; u < kBatch; ++u) {
-                    m[u] = fabsf(v[u][0]);
+                    if constexpr (sizeof(T) == 4) {
+                        const uint4 a = raw[u][0], c = raw[u][kRaw - 1];
+                        v[u][0] = __uint_as_float(a.x); v[u][1] = __uint_as_float(a.y); v[u][2] = __uint_as_float(a.z); v[u][3] = __uint_as_float(a.w);
+                        v[u][4] = __uint_as_float(c.x); v[u][5] = __uint_as_float(c.y); v[u][6] = __uint_as_float(c.z); v[u][7] = __uint_as_float(c.w);
+                    } else {
+                        const uint32_t a[4] = {raw[u][0].x, raw[u][0].y, raw[u][0].z, raw[u][0].w};
 #pragma unroll
-                    for (int e = 1; e < 8; ++e) m[u] = fmaxf(m[u], fabsf(v[u][e]));
-                    m[u] = fmaxf(m[u], 0.f);
+                        for (int k = 0; k < 4; ++k) { v[u][2 * k] = __uint_as_float(a[k] << 16); v[u][2 * k + 1] = __uint_as_float(a[k] & 0xFFFF0000u); }
+                    }
                 }
+                if (__any_sync(0xFFFFFFFFu, odd)) {
 #pragma unroll
-                for (int d = 8; d > 0; d >>= 1)
+                    for (int u = 0; u < kBatch; ++u) {
+                        const int i = i0 + 16 * u, b = (int)((uint32_t)i * recip >> 16), r = i - b * rows;
+                        const int64_t c = (int64_t)(kb0 + b) * kF8Block + l * 8;
+                        if (i < items && (!p.xvec || c + 8 > p.K))
 #pragma unroll
-                    for (int u = 0; u < kBatch; ++u) m[u] = fmaxf(m[u], __shfl_xor_sync(0xFFFFFFFFu, m[u], d));
+                            for (int e = 0; e < 8; ++e) v[u][e] = c + e < p.K ? (float)X[r * p.ldx + c + e] : 0.f;
+                    }
+                }
+                auto largest = [&]() {
+#pragma unroll
+                    for (int u = 0; u < kBatch; ++u) {
+                        m[u] = fmaxf(0.f, fabsf(v[u][0]));
+#pragma unroll
+                        for (int e = 1; e < 8; ++e) m[u] = fmaxf(m[u], fabsf(v[u][e]));
+                    }
+#pragma unroll
+                    for (int d = 8; d > 0; d >>= 1)
+#pragma unroll
+                        for (int u = 0; u < kBatch; ++u) m[u] = fmaxf(m[u], __shfl_xor_sync(0xFFFFFFFFu, m[u], d));
+                };
+                largest();
+                float top = m[0];
+#pragma unroll
+                for (int u = 1; u < kBatch; ++u) top = fmaxf(top, m[u]);
+                if (__any_sync(0xFFFFFFFFu, top == __uint_as_float(0x7F800000u))) {        // (infinities become NaN and enter no scale)
+#pragma unroll
+                    for (int u = 0; u < kBatch; ++u)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (fabsf(v[u][e]) == __uint_as_float(0x7F800000u)) v[u][e] = __uint_as_float(0x7FFFFFFFu);
+                    largest();
+                }
 #pragma unroll
                 for (int u = 0; u < kBatch; ++u) {
                     const int i = i0 + 16 * u, b = (int)((uint32_t)i * recip >> 16), r = i - b * rows;
-                    if (__any_sync(0xFFFFFFFFu, m[u] == __uint_as_float(0x7F800000u))) {        // (infinities become NaN and enter no scale)
-                        m[u] = 0.f;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            if (fabsf(v[u][e]) == __uint_as_float(0x7F800000u)) v[u][e] = __uint_as_float(0x7FFFFFFFu);
-                            m[u] = fmaxf(m[u], fabsf(v[u][e]));
-                        }
-#pragma unroll
-                        for (int d = 8; d > 0; d >>= 1) m[u] = fmaxf(m[u], __shfl_xor_sync(0xFFFFFFFFu, m[u], d));
-                    }
                     const uint32_t byte = f8_scale_byte<false>(__float_as_uint(m[u]));
                     const float f = f8_inverse(byte);
                     if (i < items) {
@@ -310,7 +328,8 @@ __global__ void __launch_bounds__(kFsThreads, std::is_same_v<T, void> ? 1 : 2) g
                 }
             }
             };
-            if (items <= 32) pass(std::integral_constant<int, 2>()); else pass(std::integral_constant<int, 8>());
+            if (items <= 32) pass(std::integral_constant<int, 2>());
+            else pass(std::integral_constant<int, 4>());               // (64 items 1.2 us; eight at a time did not fit the registers of half an SM)
             asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
             __syncwarp();
             if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(sm32(&tail.x_ready)) : "memory");
@@ -875,8 +894,8 @@ bsp_status launch_pairs(const bsp_f8 &x, const bsp_f8 &w, const float *bias, con
 
 namespace {
 
-// What a device has room for: SMs, and clusters of 1, 2, 4 and 8 CTAs of the tile kernel at a time.
-struct FsDevice { int sms, clusters[4]; };
+// What a device has room for: SMs, and clusters of 1, 2, 4 and 8 CTAs of the tile kernel at a time (those with X take half of an SM).
+struct FsDevice { int sms, clusters[4], clusters_x[4]; };
 bsp_status fs_device(FsDevice &d)
 {
     static std::atomic<int> state[kGtMaxDevices];          // 0 unknown, 1 being written, 2 known
@@ -901,8 +920,10 @@ bsp_status fs_device(FsDevice &d)
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(1024); cfg.blockDim = dim3(kFsThreads); cfg.dynamicSmemBytes = kFsSmem; cfg.attrs = &at; cfg.numAttrs = 1;
         BSP_CUDA_OK(cudaOccupancyMaxActiveClusters(&d.clusters[i], gemm_f8_tile_kernel<void>, &cfg));
+        cfg.dynamicSmemBytes = kFsSmem / 2 - 1024;
+        BSP_CUDA_OK(cudaOccupancyMaxActiveClusters(&d.clusters_x[i], gemm_f8_tile_kernel<float>, &cfg));
     }
-    if (d.sms < 1 || d.clusters[0] < 1) return BSP_ERR_CUDA;
+    if (d.sms < 1 || d.clusters[0] < 1 || d.clusters_x[0] < 1) return BSP_ERR_CUDA;
     int none = 0;
     if (state[dev].compare_exchange_strong(none, 1)) {
         known[dev] = d;
@@ -938,14 +959,18 @@ FsChoice fs_choose(const FsDevice &d, int64_t M, int64_t N, int n_kb, bool trans
         const int bn = widths[i];
         if (transposed ? (bn < N || (i > 0 && widths[i - 1] >= N)) : (bn > 32 && widths[i - 1] >= N) || bn < 32) continue;
         for (int j = 0; j < 4; ++j) {
-            const int split = 1 << j;
-            if (d.clusters[j] < 1 || (split > 1 && n_kb < 2 * split)) continue;
+            const int split = 1 << j, there = in_place ? d.clusters_x[j] : d.clusters[j];
+            if (there < 1 || (split > 1 && n_kb < 2 * split)) continue;
             const double tiles = (double)f8_blocks(M) * (double)((N + bn - 1) / bn);
-            const double waves = tiles <= d.clusters[j] ? 1.0 : (double)(int64_t)((tiles + d.clusters[j] - 1) / d.clusters[j]);
+            const double waves = tiles <= there ? 1.0 : (double)(int64_t)((tiles + there - 1) / there);
             const double mma = 4.0 * (32 + bn / 4 > bn / 2 ? 32 + bn / 4 : bn / 2), feed = 128.0 * (128 + (in_place ? 0 : bn)) / 50.0;
             const int kb = (n_kb + split - 1) / split;
             if (in_place && kb * bn > kFsPlaceRows) continue;
-            const double cycles = waves * (kb * (mma > feed ? mma : feed) + (split > 1 ? 6000.0 + 73.0 * bn / split : 2600.0 + 16.0 * bn));
+            const int items = kb * (int)(in_place ? N : 0);                 // rows of 128 entries of X
+            const double rows_x = items == 0 ? 0.0 : items <= 32 ? 1200.0 : 2400.0 * ((items + 63) / 64);
+            const double block = mma > feed ? mma : feed, entries = transposed ? (double)N * 128 : (double)(M < 128 ? M : 128) * bn;
+            const double alone = 3600.0 + 16.0 * bn, joined = (transposed ? 3400.0 + 60.0 * split : split == 8 ? 8000.0 : 5000.0 + 250.0 * split) + 0.47 * entries / split;
+            const double cycles = waves * (rows_x + kb * (transposed || block > 480.0 ? block : 480.0) + (split > 1 ? joined : alone));
             if (best.cycles < 0 || cycles < best.cycles) best = {bn, split, cycles};
         }
     }
@@ -1034,8 +1059,10 @@ bsp_status launch_linear_f8(const bsp_f8 &w, const void *X, bsp_dtype xtype, int
     bsp_status rc = fs_device(d);
     if (rc != BSP_OK) return rc;
     if (P <= 64) {
-        const FsChoice c = fs_choose(d, w.rows, P, (int)f8_blocks(w.cols), true, true);
-        if (c.cycles >= 0) return launch_tiles(d, FsJob{nullptr, &w, X, xtype, P, ldx, bias, nullptr, nullptr, Y, ytype, ws}, c, true, st);
+        const int n_kb = (int)f8_blocks(w.cols);
+        const FsChoice c = fs_choose(d, w.rows, P, n_kb, true, true);
+        // (another launch costs about 3500 cycles: 16 positions on 2048 x 1000 weights 4.5 us in place, 6.3 in two launches; 64 on 4096 x 4096 20 and 9.5)
+        if (c.cycles >= 0 && c.cycles <= fs_choose(d, w.rows, P, n_kb, true, false).cycles + 3500.0) return launch_tiles(d, FsJob{nullptr, &w, X, xtype, P, ldx, bias, nullptr, nullptr, Y, ytype, ws}, c, true, st);
     }
     rc = launch_quantize_f8(X, xtype, P, w.cols, ldx, nullptr, nullptr, &x, nullptr, nullptr, ws, st);
     return rc != BSP_OK ? rc : launch_gemm_f8(x, w, bias, nullptr, nullptr, Y, ytype, ws, st);

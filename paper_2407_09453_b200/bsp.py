@@ -399,53 +399,71 @@ def _row_distance(X, what):
     return max(X.stride(0), X.shape[1])
 
 
-def _whole(t, shape, what):
-    if t is not None and (tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
-        raise ValueError(f"{what}: a contiguous tensor of shape {tuple(shape)} is expected")
-
-
 class F8Layer:
     """A pruned linear layer on 8-bit tensors: its weights in both orientations and the calls of a training step and of serving
-    (marshalling only)."""
+    (marshalling only; what the library would misread is refused with a ValueError: another shape, type or device).  `positions`: the most that
+    one call of linear() may have."""
 
-    def __init__(self, O, I, bo, bi, wtype: torch.dtype, device="cuda"):
+    def __init__(self, O, I, bo, bi, wtype: torch.dtype, device="cuda", positions=1024):
         self.wd = wdesc(O, I, 1, 1, bo, bi, wtype)
-        self.O, self.I, self.device = O, I, device
+        self.O, self.I, self.wtype, self.positions = O, I, wtype, int(positions)
         self.w, self.wt = F8Matrix(O, I, device=device), F8Matrix(I, O, device=device)
+        self.device = self.w.data.device
         self.gamma = None
-        self.ws = new_workspace(256, device)
+        self.ws = new_workspace(bsp_linear_f8_workspace_bytes(self.w.m, self.positions), device)
+
+    def _mine(self, t, what, shape=None, dtype=None):
+        if t is None:
+            return
+        if t.device != self.device or (self.device.type == "cuda" and self.device.index != torch.cuda.current_device()):
+            raise ValueError(f"{what}: a tensor on {self.device}, the current device, is expected")
+        if dtype is not None and t.dtype != dtype:
+            raise ValueError(f"{what}: {dtype} is expected")
+        if shape is not None and (tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+            raise ValueError(f"{what}: a contiguous tensor of shape {tuple(shape)} is expected")
+
+    def _rows(self, X, channels, what):
+        self._mine(X, what)
+        ldx = _row_distance(X, what)
+        if X.shape[1] != channels:
+            raise ValueError(f"{what}: {channels} channels are expected")
+        return X.shape[0], ldx
 
     def quantize(self, W, gamma=None, stream=None):
         """Gamma (.) W in 8 bits; Gamma as SparseLayer.mask leaves it (None: all ones)."""
-        _whole(W, (self.O, self.I), "W")
+        self._mine(W, "W", (self.O, self.I), self.wtype)
+        if gamma is not None:
+            self._mine(gamma, "gamma", dtype=torch.uint8)
+            if gamma.numel() != (self.O // self.wd.bo) * (self.I // self.wd.bi) or not gamma.is_contiguous():
+                raise ValueError("gamma: an entry for every block is expected")
         self.gamma = gamma
         bsp_quantize_weights_f8(self.wd, W, gamma, self.w.m, self.wt.m, stream)
 
     def linear(self, X, bias, Y, stream=None):
         """Y = X W^t + bias for a layer that only answers; X in bfloat16 or float32."""
-        P, ldx = X.shape[0], _row_distance(X, "X")
-        if X.shape[1] != self.I:
-            raise ValueError(f"X: {self.I} channels are expected")
-        _whole(Y, (P, self.O), "Y")
-        need = bsp_linear_f8_workspace_bytes(self.w.m, P)
-        if self.ws.numel() < need:
-            self.ws = new_workspace(need, self.device)
+        P, ldx = self._rows(X, self.I, "X")
+        if P > self.positions:
+            raise ValueError(f"X: at most {self.positions} positions, as the layer was made for")
+        self._mine(bias, "bias", (self.O,), torch.float32)
+        self._mine(Y, "Y", (P, self.O))
         bsp_linear_f8(self.w.m, X, dtype_code(X.dtype), P, ldx, bias, Y, dtype_code(Y.dtype), self.ws, stream)
 
     def forward(self, X, act: F8Activations, bias, Y, stream=None):
         """Y = X W^t + bias; `act` holds X in 8 bits afterwards."""
-        _whole(Y, (X.shape[0], self.O), "Y")
-        bsp_quantize_f8(X, dtype_code(X.dtype), X.shape[0], X.shape[1], _row_distance(X, "X"), act.rows.m, act.cols.m, None, act.ws, stream)
+        P, ldx = self._rows(X, self.I, "X")
+        self._mine(bias, "bias", (self.O,), torch.float32)
+        self._mine(Y, "Y", (P, self.O))
+        bsp_quantize_f8(X, dtype_code(X.dtype), P, self.I, ldx, act.rows.m, act.cols.m, None, act.ws, stream)
         bsp_gemm_f8(act.rows.m, self.w.m, bias, Y, dtype_code(Y.dtype), self.ws, stream)
 
     def backward(self, dY, act: F8Activations, grad: F8Activations, dX=None, dW=None, db=None, stream=None):
         """Gradients of the input, of the kept weights and of the bias (those that are given) from dY and the checkpoint in `act`; `grad`
         holds dY in 8 bits afterwards."""
-        P = dY.shape[0]
-        _whole(dX, (P, self.I), "dX")
-        _whole(dW, (self.O, self.I), "dW")
-        _whole(db, (self.O,), "db")
-        bsp_quantize_f8(dY, dtype_code(dY.dtype), P, dY.shape[1], _row_distance(dY, "dY"), grad.rows.m if dX is not None or dW is None else None,
+        P, ldx = self._rows(dY, self.O, "dY")
+        self._mine(dX, "dX", (P, self.I))
+        self._mine(dW, "dW", (self.O, self.I), torch.float32)
+        self._mine(db, "db", (self.O,), torch.float32)
+        bsp_quantize_f8(dY, dtype_code(dY.dtype), P, self.O, ldx, grad.rows.m if dX is not None or dW is None else None,
                         grad.cols.m if dW is not None else None, db, grad.ws, stream)
         if dX is not None:
             bsp_gemm_f8(grad.rows.m, self.wt.m, None, dX, dtype_code(dX.dtype), self.ws, stream)

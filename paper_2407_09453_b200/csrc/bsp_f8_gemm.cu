@@ -104,6 +104,10 @@ __global__ void __launch_bounds__(kFsThreads, std::is_same_v<T, void> ? 1 : 2) g
     const uint32_t xs_scales = xs + (uint32_t)((kb1 - kb0) * BN * 128);      // (kX)
     const uint32_t cols = BN <= 32 ? 128u : BN <= 64 ? 256u : 512u;          // two accumulators and 64 columns of scales
 
+    // the bytes that the other CTAs of the cluster will send (lines: rows of the output in this tile; `per` of them to a CTA)
+    const int valid_n = p.N - n0 < BN ? p.N - n0 : BN, valid_m = p.M - m0 < 128 ? p.M - m0 : 128;
+    const int lines = p.transposed ? valid_n : valid_m, per = (p.transposed ? BN : 128) / split, line_bytes = p.transposed ? 512 : BN * 4;
+
     if (tid == 0) {
         for (int s = 0; s < S; ++s) {
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(sm32(&tail.full[s])), "r"(1) : "memory");
@@ -116,10 +120,19 @@ __global__ void __launch_bounds__(kFsThreads, std::is_same_v<T, void> ? 1 : 2) g
         asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(sm32(&tail.x_ready)), "r"(8) : "memory");
         asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(sm32(&tail.shares)), "r"(1) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+        if (split > 1) {
+            const int n = lines - rank * per < per ? lines - rank * per : per;
+            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(sm32(&tail.shares)), "r"(n > 0 ? (uint32_t)((split - 1) * n * line_bytes) : 0u) : "memory");
+        }
         s_fail = (ring & 1023u) == 0u ? 0u : 2u;
         asm volatile("prefetch.tensormap [%0];\n" ::"l"(&p.tma) : "memory");
         if constexpr (!kX) asm volatile("prefetch.tensormap [%0];\n" ::"l"(&p.tmb) : "memory");
     }
+    __syncwarp();
+    // The CTAs of a cluster run, with their barriers set up, once this barrier is complete: what they send each other waits for it.  It comes
+    // ahead of the allocation, and tensor memory is given back before a CTA waits for the others' shares: no CTA holds it while it
+    // waits for one that may still wait for columns, so clusters of several streams on the same SMs cannot stop one another.
+    if (split > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;\n" ::: "memory");
     if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(sm32(&tail.tmem)), "r"(cols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
@@ -138,17 +151,6 @@ __global__ void __launch_bounds__(kFsThreads, std::is_same_v<T, void> ? 1 : 2) g
     asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-    // the bytes that the other CTAs of the cluster will send
-    // (lines: rows of the output in this tile; `per` of them to a CTA)
-    const int valid_n = p.N - n0 < BN ? p.N - n0 : BN, valid_m = p.M - m0 < 128 ? p.M - m0 : 128;
-    const int lines = p.transposed ? valid_n : valid_m, per = (p.transposed ? BN : 128) / split, line_bytes = p.transposed ? 512 : BN * 4;
-    if (split > 1 && tid == 0) {
-        const int n = lines - rank * per < per ? lines - rank * per : per;
-        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(sm32(&tail.shares)), "r"(n > 0 ? (uint32_t)((split - 1) * n * line_bytes) : 0u) : "memory");
-    }
-    __syncwarp();
-    // (the CTAs of a cluster run once this barrier is complete: what they send each other waits for it)
-    if (split > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;\n" ::: "memory");
     const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, tail.tmem, 0), sf = tmem + cols - 64u;
     const bool run = __shfl_sync(0xFFFFFFFFu, s_fail, 0) == 0u;
     const uint32_t full0 = sm32(&tail.full[0]), empty0 = sm32(&tail.empty[0]);
@@ -360,8 +362,13 @@ __global__ void __launch_bounds__(kFsThreads, std::is_same_v<T, void> ? 1 : 2) g
             if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(sm32(&tail.acc_free[buf])) : "memory");
         }
     }
-    // ================= the shares to the CTAs that store them =================
+    // ================= tensor memory has been read =================
     __syncwarp();
+    if (warp == 0) {
+        asm volatile("bar.sync 2, 288;\n tcgen05.fence::after_thread_sync;\n" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(cols) : "memory");
+    } else if (warp >= 2) asm volatile("tcgen05.fence::before_thread_sync;\n bar.arrive 2, 288;\n" ::: "memory");
+    // ================= the shares to the CTAs that store them =================
     const int row = (warp & 3) * 32 + lane, grp = (warp - 2) >> 2;
     const int first = grp * (BN / 2), pieces = BN >= 32 ? BN / 32 : 1 - grp;
     const bool epilogue = warp >= 2;
@@ -510,11 +517,9 @@ __global__ void __launch_bounds__(kFsThreads, std::is_same_v<T, void> ? 1 : 2) g
         }
     }
     __syncwarp();
-    asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
     if (split > 1) asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
     else __syncthreads();
     if (s_fail == 1u && tid == 0) atomicMax(p.status, (int)BSP_ERR_TIMEOUT);
-    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(cols) : "memory");
 }
 
 // ---- large products: persistent pairs of CTAs ----
@@ -950,6 +955,7 @@ struct FsJob {
 // its loads, at about 50 bytes a clock and SM; what comes before and after was measured by phases (1023 x 2048 x 1000 and 1024 x 12544 x 256: 4600
 // cycles for 64 columns without a cluster; 7100 for 64 over four CTAs and 10700 for 128 over two, whose shares take 0.6 cycles an entry).
 struct FsChoice { int BN, split; double cycles; };
+constexpr int64_t kFsRow = 0x7FFFFF00;               // bytes of a row of Y that a tensor map's coordinates, which count bytes, reach
 constexpr int kFsPlaceRows = 768;                   // rows of 128 bytes of X that a CTA may hold where it quantises X itself
 FsChoice fs_choose(const FsDevice &d, int64_t M, int64_t N, int n_kb, bool transposed, bool in_place)
 {
@@ -992,7 +998,7 @@ bsp_status launch_tiles(const FsDevice &d, const FsJob &j, const FsChoice &c, bo
     p.tiles_n = (p.N + p.BN - 1) / p.BN;
     if (tiles_m * p.tiles_n * p.split > 0x7FFFFFFF) return BSP_ERR_SHAPE;
     const int ey = j.ytype == BSP_BF16 ? 2 : 4, kb = (p.n_kb + p.split - 1) / p.split;
-    p.staged = !transposed && p.split == 1 && p.BN >= 64 && (int64_t)p.N * ey % 16 == 0;
+    p.staged = !transposed && p.split == 1 && p.BN >= 64 && (int64_t)p.N * ey % 16 == 0 && (int64_t)p.N * ey < kFsRow;
     // ring | X in 8 bits and its scales | shares of the cluster's CTAs | scales of the stages | barriers
     p.stage_bytes = 16384 + (j.X ? 0 : p.BN * 128);
     const int x_bytes = j.X ? kb * p.BN * 128 + (kb / 4 + 2) * kF8Atom : 0, recv = p.split > 1 ? p.BN * 512 : 0;
@@ -1042,7 +1048,8 @@ bsp_status launch_gemm_f8(const bsp_f8 &x, const bsp_f8 &w, const float *bias, c
     const FsChoice c = fs_choose(d, transposed ? w.rows : x.rows, transposed ? x.rows : w.rows, n_kb, transposed, false);
     // pairs of CTAs, where a tensor map can describe the rows of Y
     const double tiles = (double)((x.rows + 255) / 256) * (double)((w.rows + 255) / 256), pairs = d.sms / 2;
-    if (!transposed && d.sms >= 2 && w.rows * (ytype == BSP_BF16 ? 2 : 4) % 16 == 0) {
+    const int64_t row = w.rows * (ytype == BSP_BF16 ? 2 : 4);
+    if (!transposed && d.sms >= 2 && row % 16 == 0 && row < kFsRow) {
         const double waves = (double)(int64_t)(tiles / pairs), rest = tiles - waves * pairs;
         const double cycles = (waves + (rest == 0.0 ? 0.0 : 2.0 * rest <= pairs ? 0.74 : 1.0)) * (n_kb * 690.0 + 1500.0) + 4500.0;
         if (cycles < c.cycles) return launch_pairs(x, w, bias, wd, gamma, Y, ytype, ws, d.sms, st);

@@ -125,5 +125,12 @@ def test_layer_refuses_tensors_that_it_would_misread():
                  lambda: lay.forward(x, None, None, torch.zeros(9, 64), S), lambda: lay.backward(y, None, None, dX=torch.zeros(8, 64), stream=S)):
         with pytest.raises(ValueError):
             call()
+    gamma = torch.ones(32, dtype=torch.uint8)
+    for call in (lambda: lay.quantize(torch.zeros(64, 32, dtype=torch.bfloat16)), lambda: lay.quantize(torch.zeros(64, 32), gamma[:31]), lambda: lay.quantize(torch.zeros(64, 32), gamma.bool()),
+                 lambda: lay.linear(x, torch.zeros(64, dtype=torch.bfloat16), y, S), lambda: lay.linear(x, torch.zeros(63), y, S), lambda: lay.linear(torch.zeros(1025, 32), None, torch.zeros(1025, 64), S),
+                 lambda: lay.backward(y, None, None, dW=torch.zeros(64, 32, dtype=torch.bfloat16), stream=S), lambda: lay.backward(y, None, None, db=torch.zeros(32), stream=S),
+                 lambda: lay.linear(x.to("meta"), None, y, S)):
+        with pytest.raises(ValueError):
+            call()
     with pytest.raises(TypeError):
         bsp.bsp_gemm_f8(bsp.wdesc(8, 8, 1, 1, 8, 8, bsp.F32), matrix(8, 8), None, y, bsp.F32, y, S)

@@ -531,6 +531,7 @@ constexpr int kFpStage = 32768;                     // 128 rows of A and 128 row
 constexpr int kFpStages = 5;
 constexpr int kFpScales = 3 * kF8Atom;          // scales of a stage: 128 rows of A, 256 rows of B
 constexpr int kFpStaging = 16384;                   // of a group: 128 rows of 128 bytes
+constexpr int kFpChunk = 16;                        // most blocks of a chunk (64 instructions: sums of 8192 entries off by 5.5e-7; 22 blocks 9.7e-7, and 5 % faster)
 constexpr int kFpSecond = 192;                      // first column of the second accumulator: the last 64 of the first lie under it
 
 struct FpParams {
@@ -539,6 +540,7 @@ struct FpParams {
     CUtensorMap tmy;              // Y as bytes, (N ey, M), box 128 bytes x 128 rows, 128-byte swizzle
     int M, N, n_kb, tiles_n, n_tiles;
     int n_wide;                   // tiles of 256 columns; the rest are halves of such
+    int chunk;                    // blocks of 128 entries that are summed in the tensor core before float32 registers take over
     uint32_t idesc, m_tn;
     const float *bias;
     const uint8_t *gamma;
@@ -569,7 +571,8 @@ __device__ __forceinline__ void fp_tile(const FpParams &p, int tile, int &mp, in
 // epilogue reads first, leave 64 columns for the scales: the next tile's MMAs start when these 64 have been read.
 // Where the tiles of the last wave leave half of the pairs idle they are halved (4096 x 4096 sums of 8192 entries, 34 tiles in the last wave of 74
 // pairs: 131 -> 125 us).
-// kF32: chunks of kFsChunk blocks are summed in the tensor core, these in registers (as above).
+// kF32: chunks of up to kFpChunk blocks are summed in the tensor core, these in registers (as above).  A change of accumulators costs about 1 us,
+// in which the last MMAs end, the columns that overlap are read and the next MMAs begin: chunks as long as the error allows and as few.
 template <bool kF32>
 __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __grid_constant__ FpParams p)
 {
@@ -656,11 +659,14 @@ __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __gri
         // ================= MMA issuer (the leader's, for both) =================
         if (run && rank == 0) {
             uint32_t slot = 0, par = 0, set = 0, unit = 0;
+            int left = 0;                 // blocks of this chunk to come
             bool ok = true, full_now = false;
             for (int tile = t_first; tile < p.n_tiles && ok; tile += t_step) {
                 const uint32_t tile_idesc = p.idesc | ((tile >= p.n_wide ? 16u : 32u) << 17);
                 for (int kb = 0; kb < n_kb; ++kb) {
-                    const bool fresh = kF32 ? kb % kFsChunk == 0 : kb == 0;
+                    const bool fresh = left == 0;
+                    if (fresh) left = p.chunk;
+                    --left;
                     if (fresh) {
                         // the accumulator before this one has been read where they overlap, and the one before that altogether
                         if (unit > 0 && !gt_poll(sm32(&tail.acc_free), (unit - 1u) & 1u)) ok = false;
@@ -698,7 +704,8 @@ __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __gri
                                    "h"((unsigned short)3), "r"(full0 + (wrap ? 0u : slot + 1u) * 8u), "r"(wrap ? par ^ 1u : par) : "memory");
                     full_now = next != 0u;
                     if (wrap) { slot = 0; par ^= 1u; } else ++slot;
-                    if (kb + 1 == n_kb || (kF32 && (kb + 1) % kFsChunk == 0)) {
+                    if (kb + 1 == n_kb || left == 0) {
+                        left = 0;
                         gt_commit_elected<true>(sm32(&tail.acc_full[unit & 1u]));
                         ++unit;
                     }
@@ -711,14 +718,14 @@ __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __gri
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kFpMany));
     if (run) {
         // ================= epilogue =================
-        // Group g takes the columns 64 g + (0 .. 63) and 128 + 64 g + (0 .. 63) of every tile; the ones that lie under the other accumulator
-        // first: the upper half of the first accumulator, the lower half of the second.
+        // The groups take 64 columns (128 bytes of bfloat16; 32 of float32) in turn, first the ones that lie under the other accumulator: the
+        // upper end of the first accumulator, the lower end of the second.
         const int q = warp & 3, grp = (warp - 4) >> 2, row = q * 32 + lane;
         const uint32_t sg = staging + (uint32_t)(grp * kFpStaging), lanes = (uint32_t)(q * 32) << 16;
         const bool issuer = q == 0 && lane == 0;
         const float *bias_of = from_here(p.bias);
         const uint8_t *gamma = from_here(p.gamma);
-        const int chunks = kF32 ? (n_kb + kFsChunk - 1) / kFsChunk : 1;
+        const int chunks = kF32 ? (n_kb + p.chunk - 1) / p.chunk : 1;
         uint32_t unit = 0;
         bool ok = true;
         auto hand_back = [&]() {
@@ -732,7 +739,7 @@ __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __gri
             fp_tile(p, tile, mp, n0, narrow);
             const int m0 = (2 * mp + (int)rank) * 128, m = m0 + row;
             {   // the bias of the group's 128 columns (everybody is past the barriers of the last tile's rounds)
-                const int n = n0 + (row >> 6) * 128 + grp * 64 + (row & 63);
+                const int n = n0 + (kF32 ? (row >> 5) * 64 + grp * 32 + (row & 31) : (row >> 6) * 128 + grp * 64 + (row & 63));
                 const float b = bias_of != nullptr && n < p.N ? __uint_as_float(load_free((const uint32_t *)bias_of + n)) : 0.f;
                 tail.bias[grp][row] = b;
             }
@@ -752,37 +759,36 @@ __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __gri
             if constexpr (kF32) {
                 float acc[4][32];
                 for (int c = 0; c < chunks; ++c, ++unit) {
-                    const uint32_t second = unit & 1u, t = tmem + lanes + second * kFpSecond + (uint32_t)grp * 64u;
+                    const uint32_t second = unit & 1u, t = tmem + lanes + second * kFpSecond + (uint32_t)grp * 32u;
                     if (s_fail) ok = false;
                     if (ok && !gt_wait(sm32(&tail.acc_full[second]), (unit >> 1) & 1u)) ok = false;
                     __syncwarp();
                     asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-                    if (second == (uint32_t)grp) hand_back();            // (this group has no column under the other accumulator)
-                    auto take = [&](auto half_c) {
-                        constexpr int half = decltype(half_c)::value;
-                        if (half == 1 && narrow) return;
+                    auto take = [&](auto r_c) {
+                        constexpr int r = decltype(r_c)::value;
+                        if (r >= 2 && narrow) return;
+                        uint32_t v[32];
+                        gt_load32(t + r * 64u, v);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            uint32_t v[16];
-                            fs_load16(t + half * 128u + k * 16u, v);
-                            float *sum = acc[half * 2 + (k >> 1)] + (k & 1) * 16;
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) sum[e] = c == 0 ? __uint_as_float(v[e]) : sum[e] + __uint_as_float(v[e]);
-                        }
+                        for (int e = 0; e < 32; ++e) acc[r][e] = c == 0 ? __uint_as_float(v[e]) : acc[r][e] + __uint_as_float(v[e]);
                     };
                     if (second) {
                         take(std::integral_constant<int, 0>());
-                        if (grp == 0) hand_back();
+                        hand_back();
                         take(std::integral_constant<int, 1>());
+                        take(std::integral_constant<int, 2>());
+                        take(std::integral_constant<int, 3>());
                     } else {
-                        take(std::integral_constant<int, 1>());
-                        if (grp == 1) hand_back();
+                        take(std::integral_constant<int, 3>());
+                        hand_back();
                         take(std::integral_constant<int, 0>());
+                        take(std::integral_constant<int, 1>());
+                        take(std::integral_constant<int, 2>());
                     }
                 }
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int c0 = (r >> 1) * 128 + grp * 64 + (r & 1) * 32;
+                    const int c0 = r * 64 + grp * 32;
                     if (r >= 2 && narrow) break;
                     uint32_t out[32];
                     const float *b = tail.bias[grp] + r * 32;
@@ -878,6 +884,8 @@ bsp_status launch_pairs(const bsp_f8 &x, const bsp_f8 &w, const float *bias, con
     p.n_wide = (int)tiles - (2 * last <= pairs_there ? last : 0);
     p.n_tiles = (int)(tiles + (tiles - p.n_wide));
     p.m_tn = gt_magic(p.tiles_n);
+    const int chunks = ey == 2 ? 1 : (p.n_kb + kFpChunk - 1) / kFpChunk;          // (bfloat16 has no use for the bits)
+    p.chunk = (p.n_kb + chunks - 1) / chunks;
     // formats, scales of 8 exponent bits, M / 128 (N / 8 by tile)
     p.idesc = ((x.type == BSP_E5M2 ? 1u : 0u) << 7) | ((w.type == BSP_E5M2 ? 1u : 0u) << 10) | (1u << 23) | (2u << 27);
     p.bias = bias;

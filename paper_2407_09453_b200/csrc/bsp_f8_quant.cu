@@ -36,6 +36,22 @@ __device__ __forceinline__ uint32_t bf16_max2(uint32_t a, uint32_t b)      // (p
     return *(const uint32_t *)&m;
 }
 
+// Two float32 operations in one instruction (the quantisers are bound by the instructions they issue: 76 % of the cycles).
+__device__ __forceinline__ void mul2(float &a, float &b, float f)
+{
+    asm("{\n .reg .b64 x, y;\n mov.b64 x, {%0, %1};\n mov.b64 y, {%2, %2};\n mul.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}\n" : "+f"(a), "+f"(b) : "f"(f));
+}
+__device__ __forceinline__ void add2(float &a, float &b, float c, float d)
+{
+    asm("{\n .reg .b64 x, y;\n mov.b64 x, {%0, %1};\n mov.b64 y, {%2, %3};\n add.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}\n" : "+f"(a), "+f"(b) : "f"(c), "f"(d));
+}
+template <bool kE5>
+__device__ __forceinline__ uint32_t q_pack2(float a, float b, float f)
+{
+    mul2(a, b, f);
+    return f8_pack<kE5>(a, b);
+}
+
 // 8 x 8 entries in registers, bfloat16 as they come (two to a word), so that four CTAs fit an SM (three: 28.2 us for 8192 x 4096 in both orientations, four 26.7).
 template <typename T>
 struct QEntries {
@@ -192,13 +208,18 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 ? 4 : 2) quantize_f8
         }
     }
     if (p.partial != nullptr) {
+        float s[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float s = 0.f;
+        for (int i = 0; i < 8; i += 2) {
+            s[i] = s[i + 1] = 0.f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s += v.at(j, i);
-            s += __shfl_xor_sync(0xFFFFFFFFu, s, 16);
-            if (lane < 16) s_sum[warp][tx * 8 + i] = s;
+            for (int j = 0; j < 8; ++j) add2(s[i], s[i + 1], v.at(j, i), v.at(j, i + 1));
+            s[i] += __shfl_xor_sync(0xFFFFFFFFu, s[i], 16);
+            s[i + 1] += __shfl_xor_sync(0xFFFFFFFFu, s[i + 1], 16);
+        }
+        if (lane < 16) {
+            *(float4 *)&s_sum[warp][tx * 8] = make_float4(s[0], s[1], s[2], s[3]);
+            *(float4 *)&s_sum[warp][tx * 8 + 4] = make_float4(s[4], s[5], s[6], s[7]);
         }
     }
     float rmax[8];
@@ -239,8 +260,8 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 ? 4 : 2) quantize_f8
             const uint32_t b = f8_scale_byte<kE5>(__float_as_uint(rmax[j]));
             const float f = f8_inverse(b);
             uint2 w;
-            w.x = f8_pack<kE5>(v.at(j, 0) * f, v.at(j, 1) * f) | f8_pack<kE5>(v.at(j, 2) * f, v.at(j, 3) * f) << 16;
-            w.y = f8_pack<kE5>(v.at(j, 4) * f, v.at(j, 5) * f) | f8_pack<kE5>(v.at(j, 6) * f, v.at(j, 7) * f) << 16;
+            w.x = q_pack2<kE5>(v.at(j, 0), v.at(j, 1), f) | q_pack2<kE5>(v.at(j, 2), v.at(j, 3), f) << 16;
+            w.y = q_pack2<kE5>(v.at(j, 4), v.at(j, 5), f) | q_pack2<kE5>(v.at(j, 6), v.at(j, 7), f) << 16;
             if (r0 + j < p.P && c0 < p.rows_pitch) *(uint2 *)(p.rows + (r0 + j) * p.rows_pitch + c0) = w;
             if (tx == 0) s_row[ty * 8 + j] = (uint8_t)b;
         }
@@ -279,8 +300,8 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 ? 4 : 2) quantize_f8
     for (int i = 0; i < 8; ++i) {
         const float f = inv[i];
         uint2 w;
-        w.x = f8_pack<kE5>(v.at(0, i) * f, v.at(1, i) * f) | f8_pack<kE5>(v.at(2, i) * f, v.at(3, i) * f) << 16;
-        w.y = f8_pack<kE5>(v.at(4, i) * f, v.at(5, i) * f) | f8_pack<kE5>(v.at(6, i) * f, v.at(7, i) * f) << 16;
+        w.x = q_pack2<kE5>(v.at(0, i), v.at(1, i), f) | q_pack2<kE5>(v.at(2, i), v.at(3, i), f) << 16;
+        w.y = q_pack2<kE5>(v.at(4, i), v.at(5, i), f) | q_pack2<kE5>(v.at(6, i), v.at(7, i), f) << 16;
         *(uint2 *)(s_cols + (tx * 8 + i) * kF8Block + ((ty ^ tx) << 3)) = w;
     }
     __syncthreads();

@@ -443,3 +443,94 @@ def test_calls_of_two_streams_side_by_side():
     for k in range(2):
         lays[k].check()
         assert all(torch.equal(y, alone[k]) for y in outs[k])
+
+
+def test_clusters_of_two_streams_side_by_side():
+    """Products that share sums over clusters, layers that quantise their rows in place and pairs of CTAs, on two streams at once, each with
+    workspaces of its own: each call gives what it gives alone."""
+    jobs = []
+    for k, (M, N, K, out) in enumerate([(144, 260, 5000, "f32"), (1024, 256, 6000, "f32"), (16, 4096, 4096, "bf16"), (300, 520, 2048, "f32"), (2304, 2304, 512, "bf16"), (40, 72, 9000, "f32")]):
+        A, _ = random_held(4300 + k, M, K, "e4m3")
+        B, _ = random_held(4320 + k, N, K, "e4m3", 0.05)
+        ws = [bsp.new_workspace(256) for _ in range(2)]
+        jobs.append((M, N, XTYPE[out], lambda s, Y, which, A=A, B=B, out=out, ws=ws: bsp.bsp_gemm_f8(A.m, B.m, None, Y, bsp.dtype_code(XTYPE[out]), ws[which], s)))
+    for k, (P, O, I) in enumerate([(1, 4096, 4096), (16, 1000, 2048)]):
+        B, _ = random_held(4340 + k, O, I, "e4m3", 0.05)
+        X = device(values(4350 + k, P, I, "bf16"), "bf16")
+        ws = [bsp.new_workspace(bsp.bsp_linear_f8_workspace_bytes(B.m, P)) for _ in range(2)]
+        jobs.append((P, O, torch.float32, lambda s, Y, which, B=B, X=X, P=P, I=I, ws=ws: bsp.bsp_linear_f8(B.m, X, bsp.BF16, P, I, None, Y, bsp.F32, ws[which], s)))
+    alone = []
+    for rows, cols, t, call in jobs:
+        alone.append(torch.full((rows, cols), -7.0, dtype=t, device="cuda"))
+        call(None, alone[-1], 0)
+    order = [j for j in range(len(jobs)) for _ in range(4)]
+    order = [order, order[::-1]]                                             # (the streams go through the jobs in opposite orders)
+    outs = [[torch.full(alone[j].shape, -7.0, dtype=alone[j].dtype, device="cuda") for j in o] for o in order]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for n in range(len(order[0])):
+        for which, s in enumerate(streams):
+            jobs[order[which][n]][3](s, outs[which][n], which)
+    torch.cuda.synchronize()
+    for which in range(2):
+        assert all(torch.equal(Y, alone[j]) for j, Y in zip(order[which], outs[which]))
+
+
+def test_linear_is_captured_into_a_graph():
+    for P, O, I in ((1, 520, 1000), (64, 264, 4096)):
+        lay = bsp.F8Layer(O, I, 8, 8, torch.float32)
+        lay.quantize(device(values(4400 + P, O, I, "f32", 0.05), "f32"))
+        X, Y = device(values(4401 + P, P, I, "bf16"), "bf16"), torch.empty((P, O), device="cuda")
+        lay.linear(X, None, Y)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            lay.linear(X, None, Y)
+        X.copy_(device(values(4402 + P, P, I, "bf16"), "bf16"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = Y.clone()
+        lay.linear(X, None, Y)
+        lay.check()
+        assert torch.equal(got, Y)
+
+
+def test_offsets_past_32_bits():
+    """Matrices of more than 2^31 bytes, and an output of more than 2^32: the last rows and columns are where they belong."""
+    P, I = 66000, 33000
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    X = torch.randn((P, I), device="cuda", dtype=torch.bfloat16, generator=g)
+    act = bsp.F8Activations(P, I)
+    bsp.bsp_quantize_f8(X, bsp.BF16, P, I, I, act.rows.m, act.cols.m, None, None)
+    for r in (0, P - 3):
+        codes, scales = f8.quantize(X[r:r + 3].float().cpu().numpy(), "e4m3")
+        assert np.array_equal(act.rows.data[r:r + 3, :I].view(torch.uint8).cpu().numpy(), codes)
+    for c in (0, I - 3):
+        codes, scales = f8.quantize(X[:, c:c + 3].T.float().cpu().numpy(), "e4m3")
+        assert np.array_equal(act.cols.data[c:c + 3, :P].view(torch.uint8).cpu().numpy(), codes)
+    back = torch.empty_like(X)
+    for m, transpose in ((act.rows, False), (act.cols, True)):
+        back.zero_()
+        bsp.bsp_dequantize_f8(m.m, back, bsp.BF16, I, transpose)
+        for r in (0, P - 2):
+            x = X[r:r + 2].double()
+            assert bool(((back[r:r + 2].double() - x).abs() <= 2.0 ** -4 * x.abs() + 2.0 ** -10 * 2.0 ** 3).all())
+    del X, back
+    M, N, K = 70000, 16400, 16
+    A, B = bsp.F8Matrix(M, K), bsp.F8Matrix(N, K)
+    for m in (A, B):
+        m.data.copy_(torch.randn(m.data.shape, device="cuda", generator=g).to(torch.float8_e4m3fn))
+        m.scale.fill_(127)
+    Y, ws = torch.empty((M, N), device="cuda"), bsp.new_workspace(256)
+    bsp.bsp_gemm_f8(A.m, B.m, None, Y, bsp.F32, ws)
+    bsp.bsp_check(ws)
+    for r in (0, M // 2, M - 2):
+        a, b = A.data[r:r + 2].double().cpu().numpy(), B.data.double().cpu().numpy()
+        want = a @ b.T
+        assert (np.abs(Y[r:r + 2].cpu().numpy() - want) <= product_bound(a, b, want, "f32")).all()
+    Z = torch.empty((M, N), device="cuda", dtype=torch.float32)
+    act = bsp.F8Matrix(N, M)
+    bsp.bsp_quantize_f8(Y, bsp.F32, M, N, N, None, act.m, None, None)
+    bsp.bsp_dequantize_f8(act.m, Z, bsp.F32, N, True)
+    assert bool(((Z[-1] - Y[-1]).abs() <= 2.0 ** -4 * Y[-1].abs() + 2.0 ** -9).all())

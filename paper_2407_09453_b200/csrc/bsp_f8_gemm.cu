@@ -402,8 +402,8 @@ __global__ void __launch_bounds__(kFsThreads, std::is_same_v<T, void> ? 1 : 2) g
             if (run && !gt_wait(sm32(&tail.shares), 0u)) atomicExch(&tail.fail, 1u);
             __syncwarp();
         }
-        // (complete once all shares have arrived everywhere: no CTA leaves while its memory is still read)
-        asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
+        // (complete once all shares have arrived everywhere: no CTA leaves while its memory is still read; nothing else passes by it)
+        asm volatile("barrier.cluster.arrive.relaxed.aligned;\n" ::: "memory");
     } else __syncthreads();
     // (without a cluster whoever gave up did so before the barrier, and all warps see the same; with one no barrier of the CTA alone follows)
     const bool fine = run && s_fail == 0u;

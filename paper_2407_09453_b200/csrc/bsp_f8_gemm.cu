@@ -531,7 +531,7 @@ constexpr int kFpStage = 32768;                     // 128 rows of A and 128 row
 constexpr int kFpStages = 5;
 constexpr int kFpScales = 3 * kF8Atom;          // scales of a stage: 128 rows of A, 256 rows of B
 constexpr int kFpStaging = 16384;                   // of a group: 128 rows of 128 bytes
-constexpr int kFpChunk = 16;                        // most blocks of a chunk (64 instructions: sums of 8192 entries off by 5.5e-7; 22 blocks 9.7e-7, and 5 % faster)
+constexpr int kFpChunk = 16;                        // most blocks of a chunk (64 instructions: sums of 8192 entries off by 5.5e-7; 22 blocks 9.7e-7)
 constexpr int kFpSecond = 192;                      // first column of the second accumulator: the last 64 of the first lie under it
 
 struct FpParams {
@@ -570,7 +570,7 @@ __device__ __forceinline__ void fp_tile(const FpParams &p, int tile, int &mp, in
 // of B; the leader issues MMAs of 256 x 256 x 32 for both.  Two accumulators of 256 columns that overlap by 64, whose columns the
 // epilogue reads first, leave 64 columns for the scales: the next tile's MMAs start when these 64 have been read.
 // Where the tiles of the last wave leave half of the pairs idle they are halved (4096 x 4096 sums of 8192 entries, 34 tiles in the last wave of 74
-// pairs: 131 -> 125 us).
+// pairs: 131 -> 125 us when this was added).
 // kF32: chunks of up to kFpChunk blocks are summed in the tensor core, these in registers (as above).  A change of accumulators costs
 // the end of the last MMAs, a read of the columns that overlap and the start of the next MMAs: as few chunks as the error allows.
 template <bool kF32>

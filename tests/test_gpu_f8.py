@@ -159,6 +159,17 @@ def test_quantize_any_alignment(dtype, off, ldx):
     assert_forms(quantize_both(view, "e4m3", None, ldx), x, "e4m3")
 
 
+def test_dequantize_transposed_many_tiles():
+    R, K = 2050, 2120
+    codes, scales = f8.quantize(values(2680, R, K, "f32"), "e4m3")
+    m, want = held(codes, scales, "e4m3"), f8.dequantize(codes, scales, "e4m3")
+    ld = 2056
+    X = torch.full((K, ld), -7.0, dtype=torch.bfloat16, device="cuda")
+    bsp.bsp_dequantize_f8(m.m, X, bsp.BF16, ld, True)
+    got = X.float().cpu().numpy()
+    assert np.array_equal(got[:, :R], want.T.astype(np.float32)) and (got[:, R:] == -7.0).all()
+
+
 def test_dequantize_every_code_and_scale():
     for ftype in ("e4m3", "e5m2"):
         codes = np.tile(np.arange(256, dtype=np.uint8), (256, 1))

@@ -396,7 +396,11 @@ class F8Activations:
 def _row_distance(X, what):
     if X.dim() != 2 or (X.stride(1) != 1 and X.shape[1] > 1):
         raise ValueError(f"{what}: a matrix whose rows are contiguous is expected")
-    return max(X.stride(0), X.shape[1])
+    if X.shape[0] <= 1:
+        return X.shape[1]
+    if X.stride(0) < X.shape[1]:                       # (an expanded gradient has distance 0: read as packed rows it would end past its storage)
+        raise ValueError(f"{what}: a matrix whose rows do not overlap is expected")
+    return X.stride(0)
 
 
 class F8Layer:

@@ -134,3 +134,28 @@ def test_layer_refuses_tensors_that_it_would_misread():
             call()
     with pytest.raises(TypeError):
         bsp.bsp_gemm_f8(bsp.wdesc(8, 8, 1, 1, 8, 8, bsp.F32), matrix(8, 8), None, y, bsp.F32, y, S)
+
+
+@pytest.mark.parametrize("P,C,stride", [(8, 32, (0, 1)), (8, 32, (4, 1)), (8, 32, (31, 1)), (2, 32, (0, 1)), (8, 1, (0, 1)), (8, 1, (0, 0))])
+def test_layer_refuses_rows_that_overlap(P, C, stride):
+    """Expanded and overlapping matrices, whose rows are fewer entries apart than they are long (the gradient of a sum over positions has
+    stride (0, 1)): no distance of rows describes them to the library."""
+    x = torch.zeros(P * 32).as_strided((P, C), stride)
+    with pytest.raises(ValueError, match="X: .*rows"):
+        bsp._row_distance(x, "X")
+    if C == 1:
+        return
+    lay, sq, y = bsp.F8Layer(64, 32, 8, 8, torch.float32, device="cpu"), bsp.F8Layer(32, 32, 8, 8, torch.float32, device="cpu"), torch.zeros(P, 64)
+    act = bsp.F8Activations(P, 32, device="cpu")
+    for call in (lambda: lay.linear(x, None, y, S), lambda: lay.forward(x, act, None, y, S), lambda: sq.backward(x, act, bsp.F8Activations(P, 32, device="cpu"), dX=torch.zeros(P, 32), stream=S)):
+        with pytest.raises(ValueError, match="rows"):
+            call()
+
+
+def test_row_distance():
+    assert bsp._row_distance(torch.zeros(8, 32), "X") == 32
+    assert bsp._row_distance(torch.zeros(8, 40)[:, :32], "X") == 40
+    assert bsp._row_distance(torch.zeros(8 * 50).as_strided((8, 1), (50, 7)), "X") == 50
+    for first in (0, 1, 32, 100):                                        # of a single row it is not used
+        assert bsp._row_distance(torch.zeros(200).as_strided((1, 32), (first, 1)), "X") >= 32
+    assert bsp._row_distance(torch.zeros(1, 32).expand(1, 32), "X") == 32

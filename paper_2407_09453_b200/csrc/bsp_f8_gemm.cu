@@ -11,6 +11,7 @@
 #include <atomic>
 #include <type_traits>
 #include "bsp_f8.cuh"
+#include "bsp_f8_tiles.cuh"
 #include "bsp_tc.cuh"
 
 namespace bsp {
@@ -878,13 +879,10 @@ bsp_status launch_pairs(const bsp_f8 &x, const bsp_f8 &w, const float *bias, con
     FpParams p = {};
     const int ey = ytype == BSP_BF16 ? 2 : 4;
     p.M = (int)x.rows; p.N = (int)w.rows; p.n_kb = (int)f8_blocks(x.cols);
-    p.tiles_n = (p.N + 255) / 256;
-    const long long tiles = (long long)((p.M + 255) / 256) * p.tiles_n;
-    if (tiles > 0x7FFFFFFF - 4096) return BSP_ERR_SHAPE;
-    // the tiles of the last wave, halved where two for each of them find pairs of their own
-    const int pairs_there = sms / 2, last = (int)(tiles % pairs_there);
-    p.n_wide = (int)tiles - (2 * last <= pairs_there ? last : 0);
-    p.n_tiles = (int)(tiles + (tiles - p.n_wide));
+    const int pairs_there = sms / 2;
+    F8PairTiles t;
+    if (!f8_pair_tiles(p.M, p.N, pairs_there, t)) return BSP_ERR_SHAPE;
+    p.tiles_n = t.across; p.n_wide = t.whole; p.n_tiles = t.all;
     p.m_tn = gt_magic(p.tiles_n);
     const int chunks = ey == 2 ? 1 : (p.n_kb + kFpChunk - 1) / kFpChunk;          // (bfloat16 has no use for the bits)
     p.chunk = (p.n_kb + chunks - 1) / chunks;
@@ -1004,9 +1002,8 @@ bsp_status launch_tiles(const FsDevice &d, const FsJob &j, const FsChoice &c, bo
     p.n_kb = (int)f8_blocks(K);
     p.atoms = f8_atoms(K);
     p.sa = (const uint8_t *)a->scale; p.sb = b ? (const uint8_t *)b->scale : nullptr;
-    const int64_t tiles_m = f8_blocks(p.M);
-    p.tiles_n = (p.N + p.BN - 1) / p.BN;
-    if (tiles_m * p.tiles_n * p.split > 0x7FFFFFFF) return BSP_ERR_SHAPE;
+    int64_t ctas;
+    if (!f8_tile_grid(p.M, p.N, p.BN, p.split, p.tiles_n, ctas)) return BSP_ERR_SHAPE;
     const int ey = j.ytype == BSP_BF16 ? 2 : 4, kb = (p.n_kb + p.split - 1) / p.split;
     p.staged = !transposed && p.split == 1 && p.BN >= 64 && (int64_t)p.N * ey % 16 == 0 && (int64_t)p.N * ey < kFsRow;
     // ring | X in 8 bits and its scales | shares of the cluster's CTAs | scales of the stages | barriers
@@ -1040,7 +1037,7 @@ bsp_status launch_tiles(const FsDevice &d, const FsJob &j, const FsChoice &c, bo
     if (rc == BSP_OK && p.staged) rc = fs_y_map(&p.tmy, j.Y, p.M, (int64_t)p.N * ey);
     if (rc != BSP_OK) return rc;
     const auto kernel = !j.X ? gemm_f8_tile_kernel<void> : j.xtype == BSP_F32 ? gemm_f8_tile_kernel<float> : gemm_f8_tile_kernel<__nv_bfloat16>;
-    BSP_CUDA_OK(launch_after_clusters(kernel, dim3((unsigned)(tiles_m * p.tiles_n * p.split)), dim3(kFsThreads), (size_t)smem, st, p.split, 1, p));
+    BSP_CUDA_OK(launch_after_clusters(kernel, dim3((unsigned)ctas), dim3(kFsThreads), (size_t)smem, st, p.split, 1, p));
     return BSP_OK;
 }
 

@@ -433,6 +433,13 @@ class F8Layer:
             raise ValueError(f"{what}: {channels} channels are expected")
         return X.shape[0], ldx
 
+    def _buffers(self, a, P, channels, what):
+        rows, cols = getattr(a, "rows", None), getattr(a, "cols", None)
+        if not isinstance(rows, F8Matrix) or not isinstance(cols, F8Matrix) or (rows.rows, rows.cols, cols.rows, cols.cols) != (P, channels, channels, P):
+            raise ValueError(f"{what}: F8Activations of {P} positions and {channels} channels are expected")
+        if rows.data.device != self.device or cols.data.device != self.device:
+            raise ValueError(f"{what}: buffers on {self.device} are expected")
+
     def quantize(self, W, gamma=None, stream=None):
         """Gamma (.) W in 8 bits; Gamma as SparseLayer.mask leaves it (None: all ones)."""
         self._mine(W, "W", (self.O, self.I), self.wtype)
@@ -457,6 +464,7 @@ class F8Layer:
         P, ldx = self._rows(X, self.I, "X")
         self._mine(bias, "bias", (self.O,), torch.float32)
         self._mine(Y, "Y", (P, self.O))
+        self._buffers(act, P, self.I, "act")
         bsp_quantize_f8(X, dtype_code(X.dtype), P, self.I, ldx, act.rows.m, act.cols.m, None, act.ws, stream)
         bsp_gemm_f8(act.rows.m, self.w.m, bias, Y, dtype_code(Y.dtype), self.ws, stream)
 
@@ -467,6 +475,11 @@ class F8Layer:
         self._mine(dX, "dX", (P, self.I))
         self._mine(dW, "dW", (self.O, self.I), torch.float32)
         self._mine(db, "db", (self.O,), torch.float32)
+        self._buffers(grad, P, self.O, "grad")
+        if dW is not None:
+            self._buffers(act, P, self.I, "act")
+            if grad is act or grad.cols is act.cols:
+                raise ValueError("grad: buffers other than the checkpoint's are expected")
         bsp_quantize_f8(dY, dtype_code(dY.dtype), P, self.O, ldx, grad.rows.m if dX is not None or dW is None else None,
                         grad.cols.m if dW is not None else None, db, grad.ws, stream)
         if dX is not None:

@@ -159,3 +159,23 @@ def test_row_distance():
     for first in (0, 1, 32, 100):                                        # of a single row it is not used
         assert bsp._row_distance(torch.zeros(200).as_strided((1, 32), (first, 1)), "X") >= 32
     assert bsp._row_distance(torch.zeros(1, 32).expand(1, 32), "X") == 32
+
+
+def test_layer_takes_buffers_of_the_right_size_and_device_only():
+    """What a step keeps in 8 bits, `act` and `grad`: made for other sizes, on another device, missing or one in place of the other, they are
+    refused before anything is enqueued."""
+    P, O, I = 8, 64, 32
+    lay = bsp.F8Layer(O, I, 8, 8, torch.float32, device="cpu")
+    held = lambda p, c, d="cpu": bsp.F8Activations(p, c, device=d)  # noqa: E731
+    x, y, dy, dx, dw = torch.zeros(P, I), torch.zeros(P, O), torch.zeros(P, O), torch.zeros(P, I), torch.zeros(O, I)
+    act, grad = held(P, I), held(P, O)
+    forward = lambda a: lay.forward(x, a, None, y, S)  # noqa: E731
+    backward = lambda a, g, **k: lay.backward(dy, a, g, stream=S, **k)  # noqa: E731
+    calls = [lambda a=a: forward(a) for a in (None, held(P + 1, I), held(P, I + 8), held(P, I, "meta"), act.rows)]
+    calls += [lambda g=g: backward(act, g, dX=dx) for g in (None, held(P + 1, O), held(P, O + 8), held(P, O, "meta"), act)]
+    calls += [lambda a=a: backward(a, grad, dX=dx, dW=dw) for a in (None, held(P + 1, I), held(P, I + 8), held(P, I, "meta"))]
+    square, both = bsp.F8Layer(I, I, 8, 8, torch.float32, device="cpu"), held(P, I)
+    calls.append(lambda: square.backward(x, both, both, dW=torch.zeros(I, I), stream=S))         # dY would be written over the checkpoint
+    for call in calls:
+        with pytest.raises(ValueError):
+            call()

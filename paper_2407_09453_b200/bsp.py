@@ -8,6 +8,7 @@ fails loudly if the library is missing.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 
@@ -139,6 +140,16 @@ def _stream(stream=None):
     if _raw_stream is None or _raw_device is None:
         return torch.cuda.current_stream().cuda_stream
     return _raw_stream(_raw_device())
+
+
+def _on(stream=None):
+    """The context in which PyTorch's own operations go to a stream as the calls here take it."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        raw = stream.cuda_stream
+        stream = torch.cuda.ExternalStream(raw) if raw else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
 
 
 def _raise(rc, what):
@@ -414,6 +425,7 @@ class F8Layer:
         self.w, self.wt = F8Matrix(O, I, device=device), F8Matrix(I, O, device=device)
         self.device = self.w.data.device
         self.gamma = None
+        self._gamma = torch.empty((O // bo) * (I // bi), dtype=torch.uint8, device=device)
         self.ws = new_workspace(bsp_linear_f8_workspace_bytes(self.w.m, self.positions), device)
 
     def _mine(self, t, what, shape=None, dtype=None):
@@ -441,14 +453,19 @@ class F8Layer:
             raise ValueError(f"{what}: buffers on {self.device} are expected")
 
     def quantize(self, W, gamma=None, stream=None):
-        """Gamma (.) W in 8 bits; Gamma as SparseLayer.mask leaves it (None: all ones)."""
+        """Gamma (.) W in 8 bits; Gamma as SparseLayer.mask leaves it (None: all ones).  The layer keeps a copy, so that the gradient is that of
+        these weights although the mask is taken again before backward()."""
         self._mine(W, "W", (self.O, self.I), self.wtype)
         if gamma is not None:
             self._mine(gamma, "gamma", dtype=torch.uint8)
             if gamma.numel() != (self.O // self.wd.bo) * (self.I // self.wd.bi) or not gamma.is_contiguous():
                 raise ValueError("gamma: an entry for every block is expected")
-        self.gamma = gamma
         bsp_quantize_weights_f8(self.wd, W, gamma, self.w.m, self.wt.m, stream)
+        self.gamma = None
+        if gamma is not None:
+            with _on(stream):
+                self._gamma.copy_(gamma.view(-1), non_blocking=True)
+            self.gamma = self._gamma
 
     def linear(self, X, bias, Y, stream=None):
         """Y = X W^t + bias for a layer that only answers; X in bfloat16 or float32."""

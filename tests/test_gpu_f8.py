@@ -545,3 +545,36 @@ def test_offsets_past_32_bits():
     bsp.bsp_quantize_f8(Y, bsp.F32, M, N, N, None, act.m, None, None)
     bsp.bsp_dequantize_f8(act.m, Z, bsp.F32, N, True)
     assert bool(((Z[-1] - Y[-1]).abs() <= 2.0 ** -4 * Y[-1].abs() + 2.0 ** -9).all())
+
+
+@pytest.mark.parametrize("stream", [False, True])
+def test_gradient_is_under_the_gamma_that_the_weights_were_quantised_under(stream):
+    """The mask builder writes a new Gamma to its buffer between quantize() and backward(): the gradient is still that of the layer whose
+    weights answered."""
+    P, O, I = 100, 64, 48
+    w, x, dy, _ = step_tensors(P, O, I)
+    W, X, dY = device(w, "f32"), device(x, "bf16"), device(dy, "bf16")
+    prune = bsp.SparseLayer(O, I, 1, 1, 8, 8, torch.float32)
+    lay = bsp.F8Layer(O, I, 8, 8, torch.float32)
+    act, grad = bsp.F8Activations(P, I), bsp.F8Activations(P, O)
+    Y, dW = torch.empty((P, O), device="cuda"), torch.empty((O, I), device="cuda")
+    s = torch.cuda.Stream() if stream else None
+    torch.cuda.synchronize()
+    prune.mask(W, 24, stream=s)
+    lay.quantize(W, prune.gamma, s)
+    first = prune.gamma.clone() if s is None else None
+    prune.mask(-W.flip(0).contiguous(), 24, stream=s)
+    lay.forward(X, act, None, Y, s)
+    lay.backward(dY, act, grad, dW=dW, stream=s)
+    torch.cuda.synchronize()
+    if first is None:
+        prune.mask(W, 24)
+        first = prune.gamma.clone()
+    keep = f8.spread_gamma(first.cpu().numpy(), O, I, 8, 8)
+    a, b = f8.dequantize(*f8.quantize(dy.T, "e4m3"), "e4m3"), f8.dequantize(*f8.quantize(x.T, "e4m3"), "e4m3")
+    want = np.where(keep, a @ b.T, 0.0)
+    assert (np.abs(dW.cpu().numpy() - want) <= product_bound(a, b, want, "f32")).all()
+    lay.quantize(W)                                                      # without a Gamma all weights have a gradient
+    lay.forward(X, act, None, Y)
+    lay.backward(dY, act, grad, dW=dW)
+    assert (np.abs(dW.cpu().numpy() - a @ b.T) <= product_bound(a, b, a @ b.T, "f32")).all()

@@ -117,7 +117,8 @@ def status_string(status: int) -> str:
     return lib().bsp_status_string(C.c_int(status)).decode()
 
 
-_TORCH_DT = {torch.float32: F32, torch.bfloat16: BF16, torch.int8: I8, torch.int32: I32, torch.float8_e4m3fn: E4M3, torch.float8_e5m2: E5M2}
+_TORCH_DT = {torch.float32: F32, torch.bfloat16: BF16, torch.int8: I8, torch.int32: I32}
+_TORCH_F8 = {torch.float8_e4m3fn: E4M3, torch.float8_e5m2: E5M2}          # of 8-bit matrices; tensors of plain entries have none of them
 
 
 def dtype_code(t: torch.dtype) -> int:
@@ -260,7 +261,7 @@ def bsp_f8_scale_bytes(rows: int, cols: int) -> int:
 
 def f8matrix(ftype, rows, cols, data, scale) -> F8:
     """The handle of an 8-bit matrix that lies in tensors of the caller's (bsp_f8 of include/bsp.h says how), which it keeps alive."""
-    m = F8(ftype if isinstance(ftype, int) else dtype_code(ftype), rows, cols, _ptr(data), _ptr(scale))
+    m = F8(ftype if isinstance(ftype, int) else _TORCH_F8[ftype], rows, cols, _ptr(data), _ptr(scale))
     m.tensors = data, scale
     return m
 

@@ -179,3 +179,16 @@ def test_layer_takes_buffers_of_the_right_size_and_device_only():
     for call in calls:
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("t", [torch.float8_e4m3fn, torch.float8_e5m2])
+def test_8_bit_types_are_those_of_8_bit_matrices_only(t):
+    """A tensor of plain entries has none of them: refused where its type is named, as every type is that the library does not know."""
+    for make in (lambda: bsp.SparseLayer(64, 64, 1, 1, 8, 8, t, device="cpu"), lambda: bsp.F8Layer(64, 64, 8, 8, t, device="cpu"),
+                 lambda: bsp.wdesc(64, 64, 1, 1, 8, 8, t), lambda: bsp.dtype_code(t)):
+        with pytest.raises(KeyError):
+            make()
+    lay = bsp.SparseLayer(64, 64, 1, 1, 8, 8, torch.bfloat16, device="cpu")
+    with pytest.raises(KeyError):
+        lay.gemm(torch.zeros(8, 64, dtype=torch.bfloat16), None, torch.zeros(8, 64).to(t), S)
+    assert bsp.F8Matrix(4, 4, t, device="cpu").m.type == (bsp.E4M3 if t == torch.float8_e4m3fn else bsp.E5M2)

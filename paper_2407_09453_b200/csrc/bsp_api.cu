@@ -285,7 +285,7 @@ bsp_status check_product(const bsp_f8 *x, const bsp_f8 *w, const float *bias, co
     if (rc != BSP_OK) return rc;
     if (!Y || !ws) return BSP_ERR_NULL;
     if (ytype != BSP_F32 && ytype != BSP_BF16) return BSP_ERR_DTYPE;
-    if (x->cols != w->cols || !aligned16(Y) || (bias && !aligned4(bias))) return BSP_ERR_SHAPE;
+    if (x->cols != w->cols || !aligned16(Y) || !aligned4(ws) || (bias && !aligned4(bias))) return BSP_ERR_SHAPE;
     return BSP_OK;
 }
 }  // namespace
@@ -303,7 +303,7 @@ bsp_status bsp_quantize_f8(const void *X, bsp_dtype xtype, int64_t P, int64_t I,
     if (rc == BSP_OK) rc = check_forms(rows, cols, P, I);
     if (rc != BSP_OK) return rc;
     if (colsum && !ws) return BSP_ERR_NULL;
-    if (colsum && !aligned4(colsum)) return BSP_ERR_SHAPE;
+    if (colsum && (!aligned4(colsum) || !aligned4(ws))) return BSP_ERR_SHAPE;
     return launch_quantize_f8(X, xtype, P, I, ldx, nullptr, nullptr, rows, cols, colsum, ws, (cudaStream_t)stream);
 }
 

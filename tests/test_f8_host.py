@@ -192,3 +192,13 @@ def test_8_bit_types_are_those_of_8_bit_matrices_only(t):
     with pytest.raises(KeyError):
         lay.gemm(torch.zeros(8, 64, dtype=torch.bfloat16), None, torch.zeros(8, 64).to(t), S)
     assert bsp.F8Matrix(4, 4, t, device="cpu").m.type == (bsp.E4M3 if t == torch.float8_e4m3fn else bsp.E5M2)
+
+
+def test_misaligned_workspaces_are_refused():
+    """The quantiser writes words to its workspace, the products a status word and (the layer) 16-byte pieces: none of it off its alignment."""
+    odd, y = buffer()[2:], buffer(4096, torch.float32)
+    x, w = matrix(8, 32), matrix(64, 32)
+    refused(bsp.ERR_SHAPE, lambda: bsp.bsp_quantize_f8(y, bsp.F32, 8, 32, 32, x, None, y, odd, S))
+    refused(bsp.ERR_SHAPE, lambda: bsp.bsp_gemm_f8(x, w, None, y, bsp.F32, odd, S))
+    refused(bsp.ERR_SHAPE, lambda: bsp.bsp_gemm_f8_dw(bsp.wdesc(64, 32, 1, 1, 8, 8, bsp.F32), None, matrix(64, 100), matrix(32, 100), y, odd, S))
+    refused(bsp.ERR_SHAPE, lambda: bsp.bsp_linear_f8(w, y, bsp.F32, 8, 32, None, y, bsp.F32, odd, S))

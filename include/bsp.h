@@ -289,7 +289,7 @@ bsp_status bsp_dequantize_f8(const bsp_f8 *m, void *X, bsp_dtype xtype, int64_t 
 /* bsp_gemm_f8: Y[m][n] = bias[n] + sum_k x[m][k] w[n][k], x M x K, w N x K (the types may differ), Y dense [M][N] F32 or BF16, 16-byte aligned; bias
  *             float32 [N], may be NULL.  Forward pass: x = rows form of X, w = rows form of W.  Gradient of the input: x = rows form of dY,
  *             w = cols form of W.  Products are exact.  Sums are float32: of 32 products an instruction and of up to 2048 entries in
- *             the tensor core (to the end for a BF16 output of large products), of these and of up to eight ranges of k in registers, in an
+ *             the tensor core (8192 for a BF16 output of large products), of these and of up to eight ranges of k in registers, in an
  *             order that follows from the sizes and the GPU; one rounding to BF16 after the bias.
  * bsp_gemm_f8_dw: dW[o][i] = Gamma[o / b_o][i / b_i] * sum_p dyt[o][p] xt[i][p], float32 [O][I], 16-byte aligned: the gradient of the kept weights from
  *             the cols forms of dY (O x P) and of X (I x P, the 8-bit checkpoint of the forward pass); dropped weights get 0 whatever

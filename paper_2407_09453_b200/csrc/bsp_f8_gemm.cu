@@ -533,6 +533,9 @@ constexpr int kFpStages = 5;
 constexpr int kFpScales = 3 * kF8Atom;          // scales of a stage: 128 rows of A, 256 rows of B
 constexpr int kFpStaging = 16384;                   // of a group: 128 rows of 128 bytes
 constexpr int kFpChunk = 16;                        // most blocks of a chunk (64 instructions: sums of 8192 entries off by 5.5e-7; 22 blocks 9.7e-7)
+// ... for a bfloat16 output, whose own rounding is 2^-9: 256 instructions, off by 1.1e-5 of a sum of products of one sign (2048 entries 1.8e-6).  Without
+// an end the error grew with the sum: 6.5e-5 at 32768 entries, 8.3e-4 at 262144.  Joining costs 2 % of the time of 8192 x 16384 x 4096.
+constexpr int kFpChunkHalf = 64;
 constexpr int kFpSecond = 192;                      // first column of the second accumulator: the last 64 of the first lie under it
 
 struct FpParams {
@@ -572,11 +575,13 @@ __device__ __forceinline__ void fp_tile(const FpParams &p, int tile, int &mp, in
 // epilogue reads first, leave 64 columns for the scales: the next tile's MMAs start when these 64 have been read.
 // Where the tiles of the last wave leave half of the pairs idle they are halved (4096 x 4096 sums of 8192 entries, 34 tiles in the last wave of 74
 // pairs: 131 -> 125 us when this was added).
-// kF32: chunks of up to kFpChunk blocks are summed in the tensor core, these in registers (as above).  A change of accumulators costs
-// the end of the last MMAs, a read of the columns that overlap and the start of the next MMAs: as few chunks as the error allows.
-template <bool kF32>
+// kSums: chunks of up to kFpChunk blocks (kFpChunkHalf for a bfloat16 output) are summed in the tensor core, these in registers (as above).  A
+// change of accumulators costs the end of the last MMAs, a read of the columns that overlap and the start of the next MMAs: as few chunks as the
+// error allows, and where one is enough for a bfloat16 output it goes from tensor memory to the store without the registers in between.
+template <bool kF32, bool kSums>
 __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __grid_constant__ FpParams p)
 {
+    static_assert(kSums || !kF32, "a float32 output is joined in registers");
     extern __shared__ __align__(1024) uint8_t smem[];
     FpTail &tail = *(FpTail *)(smem + kFpStages * (kFpStage + kFpScales) + 2 * kFpStaging);
     volatile uint32_t &s_fail = tail.fail;
@@ -726,7 +731,7 @@ __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __gri
         const bool issuer = q == 0 && lane == 0;
         const float *bias_of = from_here(p.bias);
         const uint8_t *gamma = from_here(p.gamma);
-        const int chunks = kF32 ? (n_kb + p.chunk - 1) / p.chunk : 1;
+        const int chunks = kSums ? (n_kb + p.chunk - 1) / p.chunk : 1;
         uint32_t unit = 0;
         bool ok = true;
         // (Only tensor memory passes by this barrier, and the tcgen05 fences order that; a release at cluster scope also waited for the
@@ -759,10 +764,13 @@ __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __gri
                     asm volatile("cp.async.bulk.commit_group;\n" ::: "memory");
                 }
             };
-            if constexpr (kF32) {
+            if constexpr (kSums) {
+                // 32 columns of the tile at a time: a round of the stores in float32, half of one in bfloat16
+                const int own = grp * (kF32 ? 32 : 64);
+                auto at = [](int r) { return kF32 ? r * 64 : (r >> 1) * 128 + (r & 1) * 32; };
                 float acc[4][32];
                 for (int c = 0; c < chunks; ++c, ++unit) {
-                    const uint32_t second = unit & 1u, t = tmem + lanes + second * kFpSecond + (uint32_t)grp * 32u;
+                    const uint32_t second = unit & 1u, t = tmem + lanes + second * kFpSecond + (uint32_t)own;
                     if (s_fail) ok = false;
                     if (ok && !gt_wait(sm32(&tail.acc_full[second]), (unit >> 1) & 1u)) ok = false;
                     __syncwarp();
@@ -771,11 +779,27 @@ __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __gri
                         constexpr int r = decltype(r_c)::value;
                         if (r >= 2 && narrow) return;
                         uint32_t v[32];
-                        gt_load32(t + r * 64u, v);
+                        gt_load32(t + (uint32_t)at(r), v);
 #pragma unroll
                         for (int e = 0; e < 32; ++e) acc[r][e] = c == 0 ? __uint_as_float(v[e]) : acc[r][e] + __uint_as_float(v[e]);
                     };
-                    if (second) {
+                    if constexpr (!kF32) {
+                        // all 64 columns that overlap are one group's
+                        if (second == (uint32_t)grp) hand_back();
+                        if (second) {
+                            take(std::integral_constant<int, 0>());
+                            take(std::integral_constant<int, 1>());
+                            if (second != (uint32_t)grp) hand_back();
+                            take(std::integral_constant<int, 2>());
+                            take(std::integral_constant<int, 3>());
+                        } else {
+                            take(std::integral_constant<int, 2>());
+                            take(std::integral_constant<int, 3>());
+                            if (second != (uint32_t)grp) hand_back();
+                            take(std::integral_constant<int, 0>());
+                            take(std::integral_constant<int, 1>());
+                        }
+                    } else if (second) {
                         take(std::integral_constant<int, 0>());
                         hand_back();
                         take(std::integral_constant<int, 1>());
@@ -789,13 +813,27 @@ __global__ void __launch_bounds__(kFpThreads, 1) gemm_f8_pair_kernel(const __gri
                         take(std::integral_constant<int, 2>());
                     }
                 }
+                gt_group_sync(1 + grp);                                  // (the bias is there)
+                if constexpr (!kF32) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (h == 1 && narrow) break;
+                        uint32_t out[32];
+                        const float *b = tail.bias[grp] + h * 64;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            const int i = 2 * e & 31, r = 2 * h + (e >> 4);
+                            out[e] = fs_pack(acc[r][i] + b[2 * e], acc[r][i + 1] + b[2 * e + 1]);
+                        }
+                        store(out, h * 128 + own);
+                    }
+                } else
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int c0 = r * 64 + grp * 32;
+                    const int c0 = at(r) + own;
                     if (r >= 2 && narrow) break;
                     uint32_t out[32];
                     const float *b = tail.bias[grp] + r * 32;
-                    if (r == 0) gt_group_sync(1 + grp);                  // (the bias is there)
 #pragma unroll
                     for (int e = 0; e < 32; ++e) out[e] = __float_as_uint(acc[r][e] + b[e]);
                     if (gamma != nullptr && m < p.M) {
@@ -884,7 +922,7 @@ bsp_status launch_pairs(const bsp_f8 &x, const bsp_f8 &w, const float *bias, con
     if (!f8_pair_tiles(p.M, p.N, pairs_there, t)) return BSP_ERR_SHAPE;
     p.tiles_n = t.across; p.n_wide = t.whole; p.n_tiles = t.all;
     p.m_tn = gt_magic(p.tiles_n);
-    const int chunks = ey == 2 ? 1 : (p.n_kb + kFpChunk - 1) / kFpChunk;          // (bfloat16 has no use for the bits)
+    const int most = ey == 2 ? kFpChunkHalf : kFpChunk, chunks = (p.n_kb + most - 1) / most;
     p.chunk = (p.n_kb + chunks - 1) / chunks;
     // formats, scales of 8 exponent bits, M / 128 (N / 8 by tile)
     p.idesc = ((x.type == BSP_E5M2 ? 1u : 0u) << 7) | ((w.type == BSP_E5M2 ? 1u : 0u) << 10) | (1u << 23) | (2u << 27);
@@ -899,7 +937,8 @@ bsp_status launch_pairs(const bsp_f8 &x, const bsp_f8 &w, const float *bias, con
     if (rc == BSP_OK) rc = fs_y_map(&p.tmy, Y, p.M, (int64_t)p.N * ey);
     if (rc != BSP_OK) return rc;
     const int pairs = p.n_tiles < pairs_there ? p.n_tiles : pairs_there;
-    BSP_CUDA_OK(launch_after_clusters(ey == 4 ? gemm_f8_pair_kernel<true> : gemm_f8_pair_kernel<false>, dim3((unsigned)(2 * pairs)), dim3(kFpThreads), kFpSmem, st, 2, 1, p));
+    const auto kernel = ey == 4 ? gemm_f8_pair_kernel<true, true> : chunks > 1 ? gemm_f8_pair_kernel<false, true> : gemm_f8_pair_kernel<false, false>;
+    BSP_CUDA_OK(launch_after_clusters(kernel, dim3((unsigned)(2 * pairs)), dim3(kFpThreads), kFpSmem, st, 2, 1, p));
     return BSP_OK;
 }
 
@@ -924,8 +963,8 @@ bsp_status fs_device(FsDevice &d)
     BSP_CUDA_OK(cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev));
     void (*const tiles[3])(const FsParams) = {gemm_f8_tile_kernel<void>, gemm_f8_tile_kernel<float>, gemm_f8_tile_kernel<__nv_bfloat16>};
     for (auto k : tiles) BSP_CUDA_OK(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kFsSmem));
-    BSP_CUDA_OK(cudaFuncSetAttribute(gemm_f8_pair_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFpSmem));
-    BSP_CUDA_OK(cudaFuncSetAttribute(gemm_f8_pair_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFpSmem));
+    void (*const pairs[3])(const FpParams) = {gemm_f8_pair_kernel<true, true>, gemm_f8_pair_kernel<false, true>, gemm_f8_pair_kernel<false, false>};
+    for (auto k : pairs) BSP_CUDA_OK(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kFpSmem));
     for (int i = 0; i < 4; ++i) {
         cudaLaunchAttribute at = {};
         at.id = cudaLaunchAttributeClusterDimension;

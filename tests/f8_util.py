@@ -1,4 +1,6 @@
 """Helpers for the tests of the 8-bit floating-point operators: 8-bit matrices between numpy codes and the device, inputs, tolerances."""
+import re
+
 import numpy as np
 import torch
 
@@ -50,3 +52,32 @@ def product_bound(x, w, want, out):
     bounds; and half a step of the output's type."""
     steps = -(-x.shape[1] // 32) + 9
     return steps * 2.0 ** -23 * (np.abs(x) @ np.abs(w).T) * 1.01 + EPS2[out] * np.abs(want) * 1.01 + 1e-37
+
+
+def launches(call):
+    """The kernels that `call` launches, in order, as (name, CTAs): captured into a graph, whose nodes are read and which never runs."""
+    from cuda.bindings import driver
+
+    def ok(r):
+        assert int(r[0]) == 0, r[0]
+        return r[1:] if len(r) != 2 else r[1]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(graph):
+        call()
+    raw = driver.CUgraph(int(graph.raw_cuda_graph()))
+    nodes, count = ok(driver.cuGraphGetNodes(raw, 64))
+    found = []
+    for n in nodes[:count]:
+        if ok(driver.cuGraphNodeGetType(n)) != driver.CUgraphNodeType.CU_GRAPH_NODE_TYPE_KERNEL:
+            continue
+        k = ok(driver.cuGraphKernelNodeGetParams(n))
+        name = ok(driver.cuFuncGetName(k.func)) if int(k.func) else ok(driver.cuKernelGetName(k.kern))
+        found.append((name.decode(), k.gridDimX))
+    return found
+
+
+def template(name):
+    """`kernel<arguments>` of a mangled name, arguments as mangled: ("gemm_f8_pair_kernel", "Lb1ELb1E")."""
+    m = re.search(r"\d+((?:gemm|quantize|dequantize)_f8_(?:any_)?(?:tile_|pair_)?kernel)I(.*?)EEv", name)
+    return m.groups() if m else (name, "")

@@ -6,7 +6,7 @@ import torch
 
 from oracle import f8
 from paper_2407_09453_b200 import bsp, synth
-from f8_util import FTYPE, XTYPE, codes_of, device, held, product_bound, random_held, values
+from f8_util import FTYPE, XTYPE, codes_of, device, held, launches, product_bound, random_held, template, values
 
 pytestmark = pytest.mark.gpu
 
@@ -578,3 +578,42 @@ def test_gradient_is_under_the_gamma_that_the_weights_were_quantised_under(strea
     lay.forward(X, act, None, Y)
     lay.backward(dY, act, grad, dW=dW)
     assert (np.abs(dW.cpu().numpy() - a @ b.T) <= product_bound(a, b, a @ b.T, "f32")).all()
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_long_sums_of_pairs_do_not_lose_bits(out):
+    """Products of one sign, cancelled by the bias: what is left of Y is the error of the sums.  No instruction of a sum of 8192 entries (256
+    instructions; 2048 and 64 for a float32 output) is off by more than one step of what has been summed by then, 2^-23 i / 256 of the sum, which
+    makes 128.5 steps of it; joining up to 128 of them, and the bias, half a step of the whole each."""
+    M, N, K = 2304, 2304, 262144
+    g = torch.Generator(device="cuda")
+    g.manual_seed(11)
+    A, B = bsp.F8Matrix(M, K), bsp.F8Matrix(N, K)
+    A.data.view(torch.uint8).copy_(torch.randint(0x30, 0x40, (1, K), device="cuda", dtype=torch.uint8, generator=g).expand(M, K))
+    B.data.view(torch.uint8).copy_(torch.randint(0x30, 0x40, (N, K), device="cuda", dtype=torch.uint8, generator=g))
+    for m in (A, B):
+        m.scale.fill_(127)
+    a = A.data[0].double()
+    exact = torch.cat([B.data[n:n + 128].double() @ a for n in range(0, N, 128)])
+    bias = (-exact).float()
+    Y, ws = torch.empty((M, N), dtype=XTYPE[out], device="cuda"), bsp.new_workspace(256)
+    call = lambda: bsp.bsp_gemm_f8(A.m, B.m, bias, Y, bsp.dtype_code(XTYPE[out]), ws)  # noqa: E731
+    call()
+    bsp.bsp_check(ws)
+    assert [template(n)[0] for n, _ in launches(call)] == ["gemm_f8_pair_kernel"]
+    instructions, joined = (256, 32) if out == "bf16" else (64, 128)
+    bound = ((instructions + 1) / 2 * 2.0 ** -23 + (joined + 1) * 2.0 ** -24) * 1.01
+    left = (Y.double() - (exact + bias.double())).abs() / exact
+    assert float(left.max()) <= bound, (float(left.max()), bound)
+
+
+@pytest.mark.parametrize("M,N,K,at,bt", [(1500, 1480, 8193, "e4m3", "e4m3"), (2300, 2056, 8300, "e5m2", "e4m3"), (1500, 1480, 16500, "e4m3", "e5m2"), (2300, 2056, 16400, "e4m3", "e4m3")])
+def test_gemm_bf16_in_several_sums(M, N, K, at, bt):
+    """bfloat16 outputs of pairs whose sums are joined in registers: two and three chunks a tile, whole and halved tiles, one and two tiles a pair."""
+    A, a = random_held(3080 + M, M, K, at)
+    B, b = random_held(3180 + K, N, K, bt, 0.05)
+    bias = synth.normal(3280, (N,), 1.0).astype(np.float32)
+    got, want = gemm(A, a, B, b, bias, "bf16")
+    assert (np.abs(got - want) <= product_bound(a, b, want, "bf16")).all()
+    Y, ws = torch.empty((M, N), dtype=torch.bfloat16, device="cuda"), bsp.new_workspace(256)
+    assert [template(n) for n, _ in launches(lambda: bsp.bsp_gemm_f8(A.m, B.m, None, Y, bsp.BF16, ws))] == [("gemm_f8_pair_kernel", "Lb0ELb1E")]

@@ -382,8 +382,8 @@ __device__ __forceinline__ void d_load(const uint8_t *p, uint32_t (&w)[kBytes / 
 // A tile of 128 x 128 per CTA, 64 entries a thread, in stores of 16 bytes that lie side by side.  As it lies: a thread takes 16 bytes of X
 // of eight rows (16 of float32), whose lanes cover 128 columns.  Transposed: of as many columns, and a warp covers 64 rows x 32 columns,
 // so that it reads whole sectors of 32 bytes and writes 128 bytes of a row of X or more at once.
-// kWide (bfloat16, transposed; 128 threads): 128 entries a thread, so that a warp covers 128 rows and writes 256 bytes side by side: 11.8 -> 10.1 us
-// for 4096 x 4096, but 2.2 -> 2.6 for 64 x 2048, whose few CTAs have fewer threads then.
+// kWide (bfloat16, transposed; 128 threads): 128 entries a thread, so that a warp covers 128 rows and writes 256 bytes side by side: 11.7 -> 10.1 us
+// for 4096 x 4096, but 2.2 -> 2.6 for 64 x 2048, whose few CTAs have fewer threads then (kWideTiles).
 template <typename T, bool kE5, bool kTranspose, bool kWide>
 __global__ void __launch_bounds__(256) dequantize_f8_kernel(const DParams p)
 {
@@ -518,7 +518,11 @@ __global__ void __launch_bounds__(256) dequantize_f8_any_kernel(const DParams p)
     }
 }
 
-constexpr int64_t kWideTiles = 256;                 // tiles from which the wide form of the transposed bfloat16 restore is taken
+// Tiles above which the wide form of the transposed bfloat16 restore is taken: two for each of 148 SMs, as many CTAs as fit beside the waiting ones of the
+// kernel that follows.  Measured on 16 to 2048 tiles, us narrow and wide, in a row and (in brackets) with another kernel between: 128 tiles 3.4 and 3.8
+// (5.6 and 6.0), 256 tiles 4.66 and 4.71 (6.8 and 6.9), 288 4.8 and 4.9 (7.0 and 7.0), 320 6.5 and 5.5 (7.8 and 7.7), 512 7.0 and 7.6 (9.2 and 8.8), 784 9.8
+// and 8.5 (12.0 and 10.6), 1024 11.7 and 10.1 (13.9 and 12.6).
+constexpr int64_t kWideTiles = 296;
 
 bool rows_of_16(const void *X, int64_t ldx, int esz) { return ((uintptr_t)X & 15u) == 0 && ldx * esz % 16 == 0; }
 
@@ -563,7 +567,7 @@ bsp_status launch_dequantize_f8(const bsp_f8 &m, void *X, bsp_dtype xtype, int64
          {dequantize_f8_kernel<float, true, false, false>, dequantize_f8_kernel<float, true, true, false>}},
         {{dequantize_f8_kernel<__nv_bfloat16, false, false, false>, dequantize_f8_kernel<__nv_bfloat16, false, true, false>},
          {dequantize_f8_kernel<__nv_bfloat16, true, false, false>, dequantize_f8_kernel<__nv_bfloat16, true, true, false>}}};
-    if (p.vec && transpose && xtype == BSP_BF16 && tiles >= kWideTiles) {
+    if (p.vec && transpose && xtype == BSP_BF16 && tiles > kWideTiles) {
         BSP_CUDA_OK(launch_after(m.type == BSP_E5M2 ? dequantize_f8_kernel<__nv_bfloat16, true, true, true> : dequantize_f8_kernel<__nv_bfloat16, false, true, true>,
                                  dim3((unsigned)tiles), dim3(128), 0, st, p));
         return BSP_OK;

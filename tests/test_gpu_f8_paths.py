@@ -10,7 +10,7 @@ import torch
 
 from oracle import f8
 from paper_2407_09453_b200 import bsp, synth
-from f8_util import EPS2, FTYPE, XTYPE, codes_of, device, launches, product_bound, random_held, template, values
+from f8_util import EPS2, FTYPE, XTYPE, codes_of, device, held, launches, product_bound, random_held, template, values
 
 pytestmark = pytest.mark.gpu
 
@@ -220,3 +220,16 @@ assert all(torch.equal(a, b) and bool(a.isfinite().all()) for a, b in zip(got, o
 def test_first_calls_of_a_process_are_captured():
     """No call needs one before it that is not captured."""
     subprocess.run([sys.executable, "-c", FIRST], check=True, timeout=300, cwd=ROOT)
+
+
+@pytest.mark.parametrize("R,K,wide", [(2048, 2304, False), (2056, 2300, True), (2560, 2560, True), (2048, 2304 + 128, True)])
+def test_transposed_restore_on_both_sides_of_its_rule(R, K, wide):
+    """288 tiles and 304 to 400: the same values by both forms, nothing behind the rows written."""
+    codes, scales = f8.quantize(values(5400 + R, R, K, "f32"), "e5m2")
+    m, want = held(codes, scales, "e5m2"), f8.dequantize(codes, scales, "e5m2").T
+    X = torch.full((K, R + 8), -7.0, dtype=torch.bfloat16, device="cuda")
+    call = lambda: bsp.bsp_dequantize_f8(m.m, X, bsp.BF16, R + 8, True)  # noqa: E731
+    call()
+    got = X.float().cpu().numpy()
+    assert np.array_equal(got[:, :R], want.astype(np.float32)) and (got[:, R:] == -7.0).all()
+    assert [template(n) for n, _ in launches(call)] == [("dequantize_f8_kernel", "13__nv_bfloat16Lb1ELb1ELb%dE" % wide)]

@@ -233,3 +233,38 @@ def test_transposed_restore_on_both_sides_of_its_rule(R, K, wide):
     got = X.float().cpu().numpy()
     assert np.array_equal(got[:, :R], want.astype(np.float32)) and (got[:, R:] == -7.0).all()
     assert [template(n) for n, _ in launches(call)] == [("dequantize_f8_kernel", "13__nv_bfloat16Lb1ELb1ELb%dE" % wide)]
+
+
+@pytest.mark.parametrize("P,I,O", [(1, 520, 264), (20, 272, 136), (50, 112, 264), (64, 2048, 136), (100, 300, 264)])
+def test_linear_on_e5m2_weights(P, I, O):
+    x = values(5500 + P, P, I, "bf16")
+    B, b = random_held(5501 + O, O, I, "e5m2", 0.05)
+    a = f8.dequantize(*f8.quantize(x, "e4m3"), "e4m3")
+    Y, ws = torch.full((P, O), -7.0, device="cuda"), bsp.new_workspace(bsp.bsp_linear_f8_workspace_bytes(B.m, P))
+    bsp.bsp_linear_f8(B.m, device(x, "bf16"), bsp.BF16, P, I, None, Y, bsp.F32, ws)
+    bsp.bsp_check(ws)
+    want = a @ b.T
+    assert (np.abs(Y.cpu().numpy() - want) <= product_bound(a, b, want, "f32")).all()
+
+
+def test_step_in_one_call_after_another_on_strided_and_single_rows():
+    """Views that describe themselves by their stride, and a single row whose stride says nothing, give what packed copies give."""
+    O, I = 72, 40
+    lay = bsp.F8Layer(O, I, 8, 8, torch.float32)
+    lay.quantize(device(values(5600, O, I, "f32", 0.05), "f32"))
+    wide = device(values(5601, 70, I + 24, "bf16"), "bf16")
+    for X in (wide[:, 8:8 + I], wide[::3, :I], wide[:1, :I], wide[:1, :I].expand(1, I), wide[:, :1].t()[:, :I]):
+        P = X.shape[0]
+        outs = []
+        for x in (X, X.contiguous()):
+            act, Y, Z = bsp.F8Activations(P, I), torch.empty((P, O), device="cuda"), torch.empty((P, O), device="cuda")
+            if x.stride(1) != 1:
+                with pytest.raises(ValueError):
+                    lay.linear(x, None, Z)
+                x = x.contiguous()
+            lay.forward(x, act, None, Y)
+            lay.linear(x, None, Z)
+            lay.check()
+            outs.append((Y, Z, codes_of(act.rows)))
+        (Y, Z, r), (y, z, s) = outs
+        assert torch.equal(Y, y) and torch.equal(Z, z) and np.array_equal(r[0], s[0]) and np.array_equal(r[1], s[1])

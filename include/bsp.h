@@ -251,7 +251,7 @@ bsp_status bsp_index_from_relative(int NBo, const int32_t *row_ptr, const int32_
  * An 8-bit matrix of `rows` rows of `cols` entries: entry (r, k) stands for value(r, k) * 2^(b - 127), where b is the scale byte of row r and
  * block k / 128 (127: times one; 255: NaN).
  *   type   BSP_E4M3 (largest value 448) or BSP_E5M2 (57344; the calls below write no infinity)
- *   data   [rows][bsp_f8_pitch(cols)] bytes, 16-byte aligned; what lies past `cols` in a row is never read
+ *   data   [rows][bsp_f8_pitch(cols)] bytes, 16-byte aligned; what lies past `cols` in a row enters no value
  *   scale  bsp_f8_scale_bytes() bytes, 16-byte aligned, in the order in which a tensor core takes them: with A = ceil(cols / 512) the byte of
  *          row r and block b lies at ((r / 128) A + b / 4) 512 + (r % 32) 16 + (r % 128 / 32) 4 + b % 4
  * The struct is a HOST struct; its pointers are device pointers.  Matrices that a product sums along k need blocks along k, so a tensor that
@@ -293,10 +293,11 @@ bsp_status bsp_dequantize_f8(const bsp_f8 *m, void *X, bsp_dtype xtype, int64_t 
  *             order that follows from the sizes and the GPU; one rounding to BF16 after the bias.
  * bsp_gemm_f8_dw: dW[o][i] = Gamma[o / b_o][i / b_i] * sum_p dyt[o][p] xt[i][p], float32 [O][I], 16-byte aligned: the gradient of the kept weights from
  *             the cols forms of dY (O x P) and of X (I x P, the 8-bit checkpoint of the forward pass); dropped weights get 0 whatever
- *             the sums are.  gamma may be NULL (all ones).  wd gives O, I and the block shape (its wtype is not used, H = K = 1).
+ *             the sums are.  gamma may be NULL (all ones).  wd gives O, I and the block shape (its wtype, any that a descriptor may have, is not used; H = K = 1).
  * bsp_linear_f8: Y[p][o] = bias[o] + sum_i q(X)[p][i] w[o][i], X [P][I] F32 or BF16 with rows ldx entries apart: bsp_quantize_f8 to e4m3 rows and
  *             bsp_gemm_f8 in one call, for a layer that only answers (down to a single token; few positions take one launch).
- *             ws: bsp_linear_f8_workspace_bytes() bytes.
+ *             Y does not overlap X.  ws: bsp_linear_f8_workspace_bytes() bytes; X in 8 bits lies there where the call takes two launches, so that
+ *             calls on different streams, replays of captured ones among them, need one each.
  *   ws of the two products: any workspace of at least 256 bytes (status word only).
  * Errors: NULL, SHAPE (as above; inner sizes differ; sizes of wd differ from the matrices'), BLOCK, DTYPE, CUDA, TIMEOUT (latched). */
 bsp_status bsp_gemm_f8(const bsp_f8 *x, const bsp_f8 *w, const float *bias, void *Y, bsp_dtype ytype, void *ws, void *stream);

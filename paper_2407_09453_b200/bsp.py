@@ -417,8 +417,9 @@ def _row_distance(X, what):
 
 class F8Layer:
     """A pruned linear layer on 8-bit tensors: its weights in both orientations and the calls of a training step and of serving
-    (marshalling only; what the library would misread is refused with a ValueError: another shape, type or device).  `positions`: the most that
-    one call of linear() may have."""
+    (marshalling only; what the library would misread is refused with a ValueError: another shape, type or device, rows that
+    overlap).  `positions`: the most that one call of linear() may have.  The calls of one layer share its workspace and its copy of Gamma: they
+    run on one stream, or one after another."""
 
     def __init__(self, O, I, bo, bi, wtype: torch.dtype, device="cuda", positions=1024):
         self.wd = wdesc(O, I, 1, 1, bo, bi, wtype)
